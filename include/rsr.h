@@ -29,17 +29,22 @@ enum {
     RSR_BINARY = 0,           /* M in {0,1}; one pass, 2^k patterns per block            */
     RSR_TERNARY_2PASS = 1,    /* M = M+ - M-, each half handled as a binary pass          */
     RSR_TERNARY_FUSED = 2,    /* one pass over base-3 patterns (3^k per block)            */
-    RSR_DENSE_TERNARY_P2 = 3  /* comparison point: dense 2-bit packed ternary, no RSR     */
+    RSR_DENSE_TERNARY_P2 = 3, /* comparison point: dense 2-bit packed ternary, no RSR     */
+    RSR_INT4 = 4              /* 4-bit weights with group scales (rsr_preprocess_int4)    */
 };
 
 /* element type of the activation vector v */
 enum { RSR_F32 = 0, RSR_BF16 = 1 };
 
+/* activation of a gated block: a / (1 + exp(-a)); 0.5 a (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))); max(a, 0)^2 */
+enum { RSR_SILU = 0, RSR_GELU = 1, RSR_RELU2 = 2 };
+
 /* error codes */
 enum {
     RSR_OK = 0,
     RSR_EINVAL = 1,       /* null pointer, non-positive size, unknown enum, bad handle     */
-    RSR_EVALUE = 2,       /* a matrix entry is outside the alphabet of the kind            */
+    RSR_EVALUE = 2,       /* a matrix entry is outside the alphabet of the kind (int4: also a zero point, */
+                          /* or a scale that is not finite)                                */
     RSR_EUNSUPPORTED = 3, /* valid request outside the limits stated below                 */
     RSR_ENOMEM = 4,       /* device or host allocation failed                              */
     RSR_EHIP = 5,         /* a HIP runtime call failed                                     */
@@ -126,7 +131,8 @@ int rsr_matvec(rsr_handle_t h, const void *v, void *out, void *stream);
  * gives the same bits every time.  A caller whose results must not depend on the batch that a
  * vector happens to be in makes one call per vector.
  *
- * An infinite or NaN element of a vector reaches the rows whose entry in its column is not zero; with
+ * Int4 handles multiply as rsr_int4_matvec says, with a float32 result.  For the other kinds:
+ * an infinite or NaN element of a vector reaches the rows whose entry in its column is not zero; with
  * the block patterns (one vector, and batches on few rows) it may reach the other rows of their blocks
  * too, as sums of several groups are subtracted there.  The dense kind multiplies every entry, so
  * all rows of the vector are NaN.  Other vectors of a batch are never touched.  On the matrix cores a
@@ -224,6 +230,90 @@ rsr_handle_t rsr_deserialize(const void *host_buf, int64_t size);
  */
 #define RSR_INTO_SCRATCH_BYTES (32 * 1024 * 1024)
 int rsr_preprocess_into(rsr_handle_t h, const int8_t *M);
+
+/*
+ * rsr_preprocess_int4 -- a handle of a dense matrix in 4 bits with one scale, and one zero point if there are any, per
+ * row and group of columns:
+ *
+ *     M[r][c] = scales[r][c / group] * (Q[r][c] - zeros[r][c / group])
+ *
+ *   Q       DEVICE int8 [rows][cols], entries -8..7
+ *   scales  DEVICE float32 [rows][ceil(cols / group)], finite.  Kept as bf16 if every one of them is a bf16, else as
+ *           float32: never rounded.
+ *   zeros   DEVICE int8, as scales, entries -8..7; or NULL: all zero
+ *   group   columns that share a scale: a positive multiple of 32, or any number >= cols (one scale per row); the last group
+ *           of a row may be shorter
+ *   rows <= 2^30, cols <= 2^24 (RSR_EUNSUPPORTED beyond)
+ *
+ * All three are borrowed until the call returns.  Runs on the null stream and synchronises.  An entry, zero point or scale out
+ * of range: RSR_EVALUE.
+ *
+ * The handle (kind RSR_INT4) multiplies through rsr_matvec, rsr_matvec_ex, rsr_int4_matvec and, in pairs, rsr_gated.  It has
+ * no blocks, patterns or permutation; rsr_serialize, rsr_serialized_size and rsr_preprocess_into refuse it
+ * (RSR_EUNSUPPORTED), the getters as for any other kind that has not what they return (RSR_EINVAL).
+ */
+rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int8_t *zeros, int64_t rows, int64_t cols,
+                                 int64_t group);
+
+/*
+ * rsr_int4_matvec -- products of `batch` vectors with an int4 handle's matrix or with its transpose:
+ *
+ *     out[n] = scale * M v[n]      transposed = 0: v[n] of length cols, out[n] of length rows
+ *     out[n] = scale * M^T v[n]    transposed = 1: v[n] of length rows, out[n] of length cols; for the gradient v of a
+ *                                  product's result this is the gradient of its input
+ *
+ * from the same codes; nothing else is kept for the transpose.
+ *
+ *   v, out     DEVICE pointers of v_dtype and out_dtype (RSR_F32 or RSR_BF16); out is overwritten, and rounded once.  They may
+ *              not overlap.
+ *   batch      0 (nothing to do) to 2^24; vector n starts at v + n*ldv elements, its result at out + n*ldo (each at least
+ *              the vector's length; not looked at for one vector)
+ *
+ * Sums are float32 and the weights are exact: codes minus zero points are multiplied as whole numbers and sums over
+ * a group are scaled.  The transpose sums over the rows, whose scales differ, so there it is the vector that is scaled:
+ * in float32, but rounded to bf16 (half a step, 2^-8) where v and out are both bf16; with float32 on either side nothing is
+ * rounded below float32.  Every entry is multiplied, zeros too: an infinite or NaN element of a vector
+ * leaves none of its results finite (others of the batch are never touched), and elements beyond 2^120 may.  A float32 element below
+ * 2^-109 loses its bits below 2^-133.  The order of the sums depends on the number of vectors, as for rsr_matvec_ex; the
+ * same call gives the same bits every time.
+ *
+ * Asynchronous on `stream`, allocates nothing and never synchronises, so it may be captured into a HIP graph; the
+ * current device must be the handle's.  No scratch memory: calls on different streams with different `out` may overlap.
+ */
+int rsr_int4_matvec(rsr_handle_t h, int transposed, const void *v, int v_dtype, float scale, void *out, int out_dtype,
+                    int batch, int64_t ldv, int64_t ldo, void *stream);
+
+/*
+ * rsr_gated -- the gated feed-forward block up to its last projection, in one launch: both projections of the same vectors,
+ * the activation and the product,
+ *
+ *     out[n][r] = act(a[r]) * b[r],   a = Mgate v[n],   b = Mup v[n]
+ *
+ *   gate, up   int4 handles of one shape (RSR_EINVAL otherwise) whose groups, reduced to 32, 64 or 128 columns (the widest of
+ *              these that divides `group`; 128 for one scale per row), are the same (RSR_EUNSUPPORTED otherwise); scales
+ *              and zero points of either kind on either side.  They may be the same handle.
+ *   act        RSR_SILU, RSR_GELU or RSR_RELU2
+ *   pre        DEVICE float32 [batch][2][rows], or NULL: receives a and b, which the backward pass needs
+ * The rest as for rsr_int4_matvec.
+ */
+int rsr_gated(rsr_handle_t gate, rsr_handle_t up, const void *v, int v_dtype, int act, void *out, int out_dtype,
+              float *pre, int batch, int64_t ldv, int64_t ldo, void *stream);
+
+/*
+ * rsr_gated_backward -- the gradients of rsr_gated for weights that stay as they are:
+ *
+ *     da = dout * b * act'(a),   db = dout * act(a),   dv = Mgate^T da + Mup^T db
+ *
+ *   pre    as rsr_gated wrote it
+ *   dout   DEVICE, d_dtype, [batch] vectors of length rows, ldd elements apart: the gradient of rsr_gated's result
+ *   dpre   DEVICE float32 [batch][2][rows], overwritten: da and db, which adapters beside the projections
+ *          need; may be `pre` itself, else they may not overlap
+ *   dv     DEVICE, dv_dtype, [batch] vectors of length cols, lddv apart; or NULL: only dpre is computed
+ * With a float32 dv nothing is rounded below float32; for a bf16 one da and db, scaled, are rounded to bf16 once, as above.
+ * Two launches on `stream`; the rest as for rsr_int4_matvec.
+ */
+int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, const void *dout, int d_dtype, int act,
+                       float *dpre, void *dv, int dv_dtype, int batch, int64_t ldd, int64_t lddv, void *stream);
 
 /* Frees the handle and its device buffers.  NULL is allowed. */
 void rsr_destroy(rsr_handle_t h);

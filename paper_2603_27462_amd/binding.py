@@ -16,8 +16,9 @@ import numpy as np
 
 from . import build as _build
 
-RSR_BINARY, RSR_TERNARY_2PASS, RSR_TERNARY_FUSED, RSR_DENSE_TERNARY_P2 = 0, 1, 2, 3
+RSR_BINARY, RSR_TERNARY_2PASS, RSR_TERNARY_FUSED, RSR_DENSE_TERNARY_P2, RSR_INT4 = 0, 1, 2, 3, 4
 RSR_F32, RSR_BF16 = 0, 1
+RSR_SILU, RSR_GELU, RSR_RELU2 = 0, 1, 2
 
 # every symbol include/rsr.h declares
 exported_symbols = [
@@ -28,6 +29,7 @@ exported_symbols = [
     "rsr_algorithmic_bytes",
     "rsr_kernel_name", "rsr_preprocess_into", "rsr_launch_shape", "rsr_probe_empty", "rsr_probe_read",
     "rsr_preprocess_stacked", "rsr_matvec_stacked", "rsr_num_layers", "rsr_batch_kernel_name",
+    "rsr_preprocess_int4", "rsr_int4_matvec", "rsr_gated", "rsr_gated_backward",
 ]
 
 
@@ -111,6 +113,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.rsr_kernel_name.argtypes = [vp, ci]
     lib.rsr_batch_kernel_name.restype = ctypes.c_char_p
     lib.rsr_batch_kernel_name.argtypes = [vp, ci, ci]
+    lib.rsr_preprocess_int4.restype = vp
+    lib.rsr_preprocess_int4.argtypes = [vp, vp, vp, i64, i64, i64]
+    lib.rsr_int4_matvec.restype = ci
+    lib.rsr_int4_matvec.argtypes = [vp, ci, vp, ci, cf, vp, ci, ci, i64, i64, vp]
+    lib.rsr_gated.restype = ci
+    lib.rsr_gated.argtypes = [vp, vp, vp, ci, ci, vp, ci, vp, ci, i64, i64, vp]
+    lib.rsr_gated_backward.restype = ci
+    lib.rsr_gated_backward.argtypes = [vp, vp, vp, vp, ci, ci, vp, vp, ci, ci, i64, i64, vp]
     _lib = lib
     _load_call(lib)
     return lib
@@ -345,6 +355,155 @@ def rsr_matvec_ex(h: Handle, v, scale: float = 1.0, out=None, stream=None):
     if rc:
         raise RsrError(rc, "rsr_matvec_ex")
     return out
+
+
+# ---- 4-bit weights with group scales ---------------------------------------------------------
+_ACTS = {"silu": RSR_SILU, "gelu": RSR_GELU, "relu2": RSR_RELU2}
+
+
+def rsr_preprocess_int4(Q, scales, group: int, zeros=None) -> Handle:
+    """Handle of M[r][c] = scales[r][c // group] * (Q[r][c] - zeros[r][c // group]).  Q: int8 CUDA tensor [rows][cols],
+    -8..7; scales: float32, bfloat16 or float16 [rows][ceil(cols / group)]; zeros: int8 like scales, -8..7, or None."""
+    import torch
+    if not (isinstance(Q, torch.Tensor) and Q.is_cuda and Q.dtype == torch.int8 and Q.dim() == 2):
+        raise TypeError("Q must be a 2-D int8 CUDA tensor")
+    rows, cols = Q.shape
+    group = int(group)
+    shape = (rows, -(-cols // group) if group > 0 else 0)
+    if not (isinstance(scales, torch.Tensor) and scales.device == Q.device and tuple(scales.shape) == shape and
+            scales.dtype in (torch.float32, torch.bfloat16, torch.float16)):
+        raise TypeError("scales must be a float tensor [rows][ceil(cols / group)] on the device of Q")
+    if zeros is not None and not (isinstance(zeros, torch.Tensor) and zeros.device == Q.device and
+                                  tuple(zeros.shape) == shape and zeros.dtype == torch.int8):
+        raise TypeError("zeros must be an int8 tensor [rows][ceil(cols / group)] on the device of Q")
+    with torch.cuda.device(Q.device):
+        Q, scales = Q.contiguous(), scales.detach().float().contiguous()
+        zeros = None if zeros is None else zeros.contiguous()
+        torch.cuda.current_stream().synchronize()   # they were produced on torch's stream
+        ptr = load_library().rsr_preprocess_int4(Q.data_ptr(), scales.data_ptr(),
+                                                 None if zeros is None else zeros.data_ptr(), rows, cols, group)
+    if not ptr:
+        raise RsrError(rsr_last_error(), "rsr_preprocess_int4")
+    h = Handle(ptr, rows, cols, 0, RSR_INT4)
+    h.device = Q.device
+    return h
+
+
+def _int4_device(*handles):
+    if any(h.kind != RSR_INT4 for h in handles):
+        raise TypeError("needs an int4 handle (rsr_preprocess_int4)")
+    if any(h.device != handles[0].device for h in handles):
+        raise TypeError("the handles are on different devices")
+    return handles[0].device
+
+
+def _vectors(v, length: int, device, name: str):
+    """(batch, distance, type) of vectors [length] or [batch][length]."""
+    import torch
+    if (not isinstance(v, torch.Tensor) or v.device != device or v.dim() not in (1, 2) or v.shape[-1] != length or
+            (length > 1 and v.stride(-1) != 1) or v.dtype not in (torch.float32, torch.bfloat16)):
+        raise TypeError("%s must be a float32 or bfloat16 tensor [%d] or [batch][%d] with unit inner stride on the handle's "
+                        "device" % (name, length, length))
+    batch = 1 if v.dim() == 1 else v.shape[0]
+    return batch, length if batch <= 1 else v.stride(0), _dtype_code(v)
+
+
+def _result(out, like, length: int, dtype, name: str = "out"):
+    """`out`, checked against the vectors `like`, or a new tensor for their results."""
+    import torch
+    shape = (*like.shape[:-1], length)
+    if out is None:
+        return torch.empty(shape, dtype=dtype or torch.float32, device=like.device)
+    if (tuple(out.shape) != shape or out.device != like.device or (length > 1 and out.stride(-1) != 1) or
+            out.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and out.dtype != dtype)):
+        raise TypeError("%s must be a float32 or bfloat16 tensor %s with unit inner stride on the handle's device, of the type "
+                        "asked for" % (name, list(shape)))
+    return out
+
+
+def _kept(pre, batch: int, rows: int, device, name: str):
+    import torch
+    if (not isinstance(pre, torch.Tensor) or pre.device != device or pre.dtype != torch.float32 or not pre.is_contiguous() or
+            tuple(pre.shape) != (batch, 2, rows)):
+        raise TypeError("%s must be a contiguous float32 tensor [%d][2][%d] on the handle's device" % (name, batch, rows))
+
+
+def _on(device, stream, call) -> int:
+    """call(stream pointer) with `device` the current one."""
+    if device.index == _current_device():
+        return call(_stream_ptr(stream))
+    import torch
+    with torch.cuda.device(device):
+        return call(_stream_ptr(stream))
+
+
+def rsr_int4_matvec(h: Handle, v, transposed: bool = False, scale: float = 1.0, dtype=None, out=None, stream=None):
+    """scale * M v, or scale * M^T v: v [length] or [batch][length], float32 or bfloat16, length cols (transposed: rows).
+    The result is of type `dtype`, by default float32."""
+    device = _int4_device(h)
+    length, to = (h.rows, h.cols) if transposed else (h.cols, h.rows)
+    batch, ldv, code = _vectors(v, length, device, "v")
+    out = _result(out, v, to, dtype)
+    ldo = to if batch <= 1 else out.stride(0)
+    rc = _on(device, stream, lambda s: load_library().rsr_int4_matvec(
+        h.ptr, int(bool(transposed)), v.data_ptr(), code, float(scale), out.data_ptr(), _dtype_code(out), batch, ldv, ldo,
+        s)) if batch else 0
+    if rc:
+        raise RsrError(rc, "rsr_int4_matvec")
+    return out
+
+
+def _act_code(act) -> int:
+    if act in _ACTS:
+        return _ACTS[act]
+    if act in _ACTS.values():
+        return int(act)
+    raise ValueError("act must be one of %s" % ", ".join(sorted(_ACTS)))
+
+
+def rsr_gated(gate: Handle, up: Handle, v, act="silu", dtype=None, out=None, pre=None, stream=None):
+    """act(Mgate v) * (Mup v) for v [cols] or [batch][cols]; act: "silu", "gelu" (tanh form) or "relu2".  The result
+    is of type `dtype`, by default float32.  pre: a float32 tensor [batch][2][rows] that receives both products, for
+    rsr_gated_backward."""
+    device = _int4_device(gate, up)
+    batch, ldv, code = _vectors(v, gate.cols, device, "v")
+    out = _result(out, v, gate.rows, dtype)
+    if pre is not None:
+        _kept(pre, batch, gate.rows, device, "pre")
+    ldo = gate.rows if batch <= 1 else out.stride(0)
+    act = _act_code(act)
+    rc = _on(device, stream, lambda s: load_library().rsr_gated(
+        gate.ptr, up.ptr, v.data_ptr(), code, act, out.data_ptr(), _dtype_code(out),
+        None if pre is None else pre.data_ptr(), batch, ldv, ldo, s)) if batch else 0
+    if rc:
+        raise RsrError(rc, "rsr_gated")
+    return out
+
+
+def rsr_gated_backward(gate: Handle, up: Handle, pre, dout, act="silu", dtype=None, dv=None, dpre=None, stream=None,
+                       need_dv: bool = True):
+    """(dv, dpre) of rsr_gated for the gradient dout of its result and the `pre` it wrote: dv [batch][cols] of type `dtype`, by
+    default float32 (None without need_dv), and dpre, float32 [batch][2][rows], the gradients of both products; a dpre given
+    may be `pre` itself."""
+    import torch
+    device = _int4_device(gate, up)
+    batch, ldd, code = _vectors(dout, gate.rows, device, "dout")
+    _kept(pre, batch, gate.rows, device, "pre")
+    if dpre is None:
+        dpre = torch.empty_like(pre)
+    _kept(dpre, batch, gate.rows, device, "dpre")
+    if need_dv:
+        dv = _result(dv, dout, gate.cols, dtype, "dv")
+    else:
+        dv = None
+    lddv = gate.cols if batch <= 1 or dv is None else dv.stride(0)
+    act = _act_code(act)
+    rc = _on(device, stream, lambda s: load_library().rsr_gated_backward(
+        gate.ptr, up.ptr, pre.data_ptr(), dout.data_ptr(), code, act, dpre.data_ptr(),
+        None if dv is None else dv.data_ptr(), RSR_F32 if dv is None else _dtype_code(dv), batch, ldd, lddv, s)) if batch else 0
+    if rc:
+        raise RsrError(rc, "rsr_gated_backward")
+    return dv, dpre
 
 
 _VECTORS = "v must be a CUDA tensor [cols] or [batch][cols] with unit inner stride"

@@ -13,7 +13,7 @@ INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "librsr.so")
 CALL_PATH = os.path.join(PKG_DIR, "_rsr_call.so")
 SOURCES = ["rsr_api.hip", "rsr_preprocess.hip", "rsr_matvec.hip", "rsr_packed.hip", "rsr_probe.hip",
-           "rsr_narrow.hip"]
+           "rsr_narrow.hip", "rsr_int4.hip", "rsr_int4_back.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,6 +1,6 @@
 // C ABI of librsr: argument checks, device-memory ownership, and the order of
 // the preprocessing launches.  All arithmetic of the method is in the kernels
-// (rsr_preprocess.hip, rsr_matvec.hip, rsr_narrow.hip, rsr_packed.hip).
+// (rsr_preprocess.hip, rsr_matvec.hip, rsr_narrow.hip, rsr_packed.hip, rsr_int4.hip, rsr_int4_back.hip).
 #include <cstddef>
 #include <cstring>
 #include <memory>
@@ -51,6 +51,25 @@ bool use_packed(const rsr_handle_s *h, int v_dtype, int batch, bool aligned) {
     // at 0.91 of the time or less (mean 1/1.26); at 1.0 it would be 280 with 9 wrong, the worst 1.13 times slower
     const bool sure = h->nb * batch <= 256 && batch <= 16 && h->k >= 4 && h->k <= 8 && aligned && h->cols >= 8000;
     return blocks > (sure ? 0.95f : 0.85f) * rsr::packed_few_rows_us(h, wide, batch);
+}
+
+bool is_int4(const rsr_handle_s *h) { return good(h) && h->kind == RSR_INT4; }
+bool vector_type(int dtype) { return dtype == RSR_F32 || dtype == RSR_BF16; }
+
+// What the entries on int4 handles have in common: the number of vectors, their distances and the device.
+int check_batch(const rsr_handle_s *h, int batch, int64_t ldv, int64_t in, int64_t ldo, int64_t out) {
+    if (batch < 0 || (batch > 1 && (ldv < in || ldo < out))) return RSR_EINVAL;
+    if (batch > rsr::kInt4MaxBatch) return RSR_EUNSUPPORTED;
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess) return RSR_EHIP;
+    return device == h->device ? RSR_OK : RSR_EINVAL;
+}
+
+int check_pair(const rsr_handle_s *gate, const rsr_handle_s *up, int act) {
+    if (!is_int4(gate) || !is_int4(up) || gate->rows != up->rows || gate->cols != up->cols || gate->device != up->device ||
+        act < RSR_SILU || act > RSR_RELU2)
+        return RSR_EINVAL;
+    return gate->group == up->group ? RSR_OK : RSR_EUNSUPPORTED;
 }
 
 // Whether every vector starts on a 16-byte boundary.
@@ -614,7 +633,7 @@ extern "C" {
 
 int rsr_preprocess_into(rsr_handle_t h, const int8_t *M) {
     if (!good(h) || !M) return fail(RSR_EINVAL);
-    if (h->nlayers > 0) return fail(RSR_EUNSUPPORTED);
+    if (h->nlayers > 0 || h->kind == RSR_INT4) return fail(RSR_EUNSUPPORTED);
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) return fail(RSR_EHIP);
     if (device != h->device) return fail(RSR_EINVAL);
@@ -736,7 +755,7 @@ extern "C" {
 
 int64_t rsr_serialized_size(rsr_handle_t h) {
     if (!good(h)) { fail(RSR_EINVAL); return -1; }
-    if (h->nlayers > 0) { fail(RSR_EUNSUPPORTED); return -1; }
+    if (h->nlayers > 0 || h->kind == RSR_INT4) { fail(RSR_EUNSUPPORTED); return -1; }
     int64_t total = (int64_t)sizeof(SerialHeader);
     for (const Piece &pc : pieces_of(h)) total += (int64_t)pc.bytes;
     return total;
@@ -744,7 +763,7 @@ int64_t rsr_serialized_size(rsr_handle_t h) {
 
 int rsr_serialize(rsr_handle_t h, void *host_buf, int64_t capacity) {
     if (!good(h) || !host_buf) return fail(RSR_EINVAL);
-    if (h->nlayers > 0) return fail(RSR_EUNSUPPORTED);
+    if (h->nlayers > 0 || h->kind == RSR_INT4) return fail(RSR_EUNSUPPORTED);
     const int64_t total = rsr_serialized_size(h);
     if (capacity < total) return fail(RSR_EINVAL);
     SerialHeader hd;
@@ -881,7 +900,8 @@ int rsr_matvec_ex(rsr_handle_t h, const void *v, int v_dtype, float scale, void 
     if (hipGetDevice(&device) != hipSuccess) return fail(RSR_EHIP);
     if (device != h->device) return fail(RSR_EINVAL);  // the handle's buffers live on another GPU
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    hipError_t e = use_packed(h, v_dtype, batch, vectors_aligned(v, v_dtype, ldv))
+    hipError_t e = h->kind == RSR_INT4 ? rsr::launch_int4(h, v, v_dtype, scale, out, RSR_F32, batch, ldv, ldo, s)
+                   : use_packed(h, v_dtype, batch, vectors_aligned(v, v_dtype, ldv))
                        ? rsr::launch_packed(h, v, v_dtype, scale, static_cast<float *>(out), batch, ldv, ldo, s)
                    : h->narrow
                        ? rsr::launch_narrow_matvec(h, v, v_dtype, scale, static_cast<float *>(out), batch, ldv,
@@ -890,6 +910,86 @@ int rsr_matvec_ex(rsr_handle_t h, const void *v, int v_dtype, float scale, void 
                                                 batch, ldv, ldo, s);
     if (e != hipSuccess) return fail(hip_code(e));
     return RSR_OK;
+}
+
+rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int8_t *zeros, int64_t rows, int64_t cols,
+                                 int64_t group) {
+    if (!Q || !scales || rows < 1 || cols < 1 || group < 1) { fail(RSR_EINVAL); return nullptr; }
+    if (rows > (int64_t)1 << 30 || cols > rsr::kInt4MaxCols || (group < cols && group % 32)) {
+        fail(RSR_EUNSUPPORTED);
+        return nullptr;
+    }
+    rsr_handle_s *h = new (std::nothrow) rsr_handle_s();
+    if (!h) { fail(RSR_ENOMEM); return nullptr; }
+    h->magic = rsr::kMagic;
+    h->kind = RSR_INT4;
+    h->rows = rows;
+    h->cols = cols;
+    h->group = group >= cols || group % 128 == 0 ? 128 : group % 64 == 0 ? 64 : 32;
+    int host[2] = {0, 0}, *flags = nullptr, rc = RSR_OK;
+    Buffers own;
+    RSR_TRY(hipGetDevice(&h->device));
+    // (the scales decide how many bytes they take)
+    RSR_TRY(dev_alloc(&flags, 2));
+    RSR_TRY(rsr::launch_fill_u32(reinterpret_cast<uint32_t *>(flags), 0u, 2));
+    RSR_TRY(rsr::launch_int4_check_scales(scales, zeros, rows * ((cols + group - 1) / group), flags));
+    RSR_TRY(hipMemcpy(host, flags, sizeof(host), hipMemcpyDeviceToHost));
+    if (host[0]) { rc = RSR_EVALUE; goto done; }
+    h->wide_scales = host[1] ? 1 : 0;
+    own.add(&h->packed, rsr::int4_code_bytes(rows, cols));
+    own.add_bytes(&h->scales, rsr::int4_groups(rows, cols, h->group) * (h->wide_scales ? 4 : 2));
+    if (zeros) own.add(&h->zeros, rsr::int4_groups(rows, cols, h->group));
+    RSR_TRY(own.allocate(h));
+    RSR_TRY(rsr::launch_int4_pack(h, Q, scales, zeros, group, flags));
+    RSR_TRY(hipMemcpy(host, flags, sizeof(host), hipMemcpyDeviceToHost));  // (waits for all of it)
+    if (host[0]) rc = RSR_EVALUE;
+done:
+    if (flags) (void)hipFree(flags);
+    if (rc != RSR_OK) {
+        (void)hipGetLastError();
+        free_handle(h);
+        fail(rc);
+        return nullptr;
+    }
+    g_last_error = RSR_OK;
+    return h;
+}
+
+int rsr_int4_matvec(rsr_handle_t h, int transposed, const void *v, int v_dtype, float scale, void *out, int out_dtype,
+                    int batch, int64_t ldv, int64_t ldo, void *stream) {
+    if (!is_int4(h) || !v || !out || !vector_type(v_dtype) || !vector_type(out_dtype)) return fail(RSR_EINVAL);
+    const int64_t in = transposed ? h->rows : h->cols, to = transposed ? h->cols : h->rows;
+    if (int rc = check_batch(h, batch, ldv, in, ldo, to)) return fail(rc);
+    if (batch == 0) return RSR_OK;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const hipError_t e =
+        transposed ? rsr::launch_int4_transposed(h, nullptr, v, v_dtype, scale, out, out_dtype, batch, ldv, ldo, s)
+                   : rsr::launch_int4(h, v, v_dtype, scale, out, out_dtype, batch, ldv, ldo, s);
+    return e == hipSuccess ? RSR_OK : fail(hip_code(e));
+}
+
+int rsr_gated(rsr_handle_t gate, rsr_handle_t up, const void *v, int v_dtype, int act, void *out, int out_dtype,
+              float *pre, int batch, int64_t ldv, int64_t ldo, void *stream) {
+    if (!v || !out || !vector_type(v_dtype) || !vector_type(out_dtype)) return fail(RSR_EINVAL);
+    if (int rc = check_pair(gate, up, act)) return fail(rc);
+    if (int rc = check_batch(gate, batch, ldv, gate->cols, ldo, gate->rows)) return fail(rc);
+    if (batch == 0) return RSR_OK;
+    const hipError_t e = rsr::launch_int4_gated(gate, up, v, v_dtype, act, out, out_dtype, pre, batch, ldv, ldo,
+                                                reinterpret_cast<hipStream_t>(stream));
+    return e == hipSuccess ? RSR_OK : fail(hip_code(e));
+}
+
+int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, const void *dout, int d_dtype, int act,
+                       float *dpre, void *dv, int dv_dtype, int batch, int64_t ldd, int64_t lddv, void *stream) {
+    if (!pre || !dout || !dpre || !vector_type(d_dtype) || (dv && !vector_type(dv_dtype))) return fail(RSR_EINVAL);
+    if (int rc = check_pair(gate, up, act)) return fail(rc);
+    if (int rc = check_batch(gate, batch, ldd, gate->rows, dv ? lddv : gate->cols, gate->cols)) return fail(rc);
+    if (batch == 0) return RSR_OK;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    hipError_t e = rsr::launch_gated_slopes(pre, dout, d_dtype, ldd, act, gate->rows, batch, dpre, s);
+    if (e == hipSuccess && dv)
+        e = rsr::launch_int4_transposed(gate, up, dpre, RSR_F32, 1.0f, dv, dv_dtype, batch, 2 * gate->rows, lddv, s);
+    return e == hipSuccess ? RSR_OK : fail(hip_code(e));
 }
 
 int rsr_probe_empty(int workgroups, int threads, int lds_bytes, void *stream) {
@@ -1015,7 +1115,10 @@ int64_t rsr_algorithmic_bytes(rsr_handle_t h, int v_dtype, int batch) {
     }
     const int64_t vb = (v_dtype == RSR_BF16) ? 2 : 4;
     int64_t weight_side;
-    if (use_packed(h, v_dtype, batch, h->cols * vb % 16 == 0)) {
+    if (h->kind == RSR_INT4) {
+        weight_side = rsr::int4_code_bytes(h->rows, h->cols) +
+                      rsr::int4_groups(h->rows, h->cols, h->group) * ((h->wide_scales ? 4 : 2) + (h->zeros ? 1 : 0));
+    } else if (use_packed(h, v_dtype, batch, h->cols * vb % 16 == 0)) {
         weight_side = rsr::packed_bytes(h->code_groups, h->cols, h->code_bits);
     } else {
         weight_side = 0;
@@ -1036,6 +1139,7 @@ const char *rsr_batch_kernel_name(rsr_handle_t h, int v_dtype, int batch) {
         return nullptr;
     }
     static thread_local char name[96];
+    if (h->kind == RSR_INT4) return "k_int4_rows";
     if (use_packed(h, v_dtype, batch, h->cols * (v_dtype == RSR_BF16 ? 2 : 4) % 16 == 0))
         rsr::packed_kernel_name(h, v_dtype, batch, name, sizeof(name));
     else if (h->narrow)

@@ -107,6 +107,11 @@ struct rsr_handle_s {
     int64_t code_groups = 0;     // row groups of 16; stacked handles: every layer starts a new one
     bool single_packed = false;  // single vectors go through the packed codes too (k = 0, timed faster)
     int64_t row_bytes = 0;       // dense kind: 64 * tiles
+    // int4 kind (rsr_int4.h): the codes are in `packed`
+    void *scales = nullptr;      // bf16 or float32
+    int8_t *zeros = nullptr;     // null: all zero
+    int wide_scales = 0;         // the scales are float32
+    int group = 0;               // columns of a group in the handle: 32, 64 or 128
 };
 
 namespace rsr {
@@ -165,6 +170,26 @@ void rsr_matvec_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char 
 void rsr_matvec_launch_shape(const rsr_handle_s *h, int v_dtype, int *threads, int *lds_bytes);
 void packed_launch_shape(const rsr_handle_s *h, int v_dtype, int *workgroups, int *threads, int *lds_bytes);
 void packed_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len);
+
+// --- 4-bit weights with group scales ------------------------------------------------------
+constexpr int64_t kInt4MaxCols = (int64_t)1 << 24;
+constexpr int kInt4MaxBatch = 1 << 24;
+int64_t int4_code_bytes(int64_t rows, int64_t cols);
+int64_t int4_groups(int64_t rows, int64_t cols, int per);  // scales of a handle with groups of `per` columns
+// Null stream; flags[0] |= 1: a value out of range, flags[1] |= 1: a scale that is no bf16.
+hipError_t launch_int4_check_scales(const float *scales, const int8_t *zeros, int64_t count, int *flags);
+hipError_t launch_int4_pack(const rsr_handle_s *h, const int8_t *Q, const float *scales, const int8_t *zeros,
+                            int64_t group, int *flags);
+hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float scale, void *out, int out_dtype,
+                       int batch, int64_t ldv, int64_t ldo, hipStream_t stream);
+hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,
+                             void *out, int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo,
+                             hipStream_t stream);
+// out[n] = scale * (a^T dy[n] + b^T dy[n] further on by a's rows); b may be null.
+hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, float scale,
+                                  void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo, hipStream_t stream);
+hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,
+                               int batch, float *dpre, hipStream_t stream);
 
 // --- narrow matrices (cols <= kNarrowCols) ---------------------------------------------
 constexpr int kNarrowCols = 256;
