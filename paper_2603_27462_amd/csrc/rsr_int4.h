@@ -51,6 +51,176 @@ __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float((uin
 __device__ __forceinline__ void put(float *at, float x) { *at = x; }
 __device__ __forceinline__ void put(uint16_t *at, float x) { *at = __builtin_bit_cast(uint16_t, (__bf16)x); }
 
+// ---- vectors ---------------------------------------------------------------------------------------
+// Eight consecutive elements, as loaded (columns past the end: zeros).
+template <typename VT>
+struct Piece {
+    u32x4 q[sizeof(VT) / 2];
+};
+
+// The piece of `row` at column `col`.
+template <typename VT>
+__device__ __forceinline__ Piece<VT> load_piece(const VT *__restrict__ row, int col, int end) {
+    Piece<VT> p = {};
+    if (col + 8 <= end) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(VT) / 2; ++i)
+            p.q[i] = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const unsigned char *>(row + col) + 16 * i);
+    } else if (col < end) {
+        uint32_t e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            e[i] = 0;
+            if (col + i < end)
+                e[i] = sizeof(VT) == 4 ? reinterpret_cast<const uint32_t *>(row)[col + i]
+                                       : reinterpret_cast<const uint16_t *>(row)[col + i];
+        }
+        if (sizeof(VT) == 4) {
+            p.q[0] = u32x4{e[0], e[1], e[2], e[3]};
+            p.q[sizeof(VT) / 2 - 1] = u32x4{e[4], e[5], e[6], e[7]};
+        } else {
+            p.q[0] = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
+        }
+    }
+    return p;
+}
+
+// low half: of a, high half: of b
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) {
+    return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
+// Writes the piece to LDS: one plane for bf16, three (`plane` bytes apart) for float32, x = top + middle + bottom 8 bits
+// exactly.
+__device__ __forceinline__ void store_piece(unsigned char *at, int, const Piece<uint16_t> &p) {
+    *reinterpret_cast<u32x4 *>(at) = p.q[0];
+}
+__device__ __forceinline__ void store_piece(unsigned char *at, int plane, const Piece<float> &p) {
+    uint32_t x[8] = {p.q[0].x, p.q[0].y, p.q[0].z, p.q[0].w, p.q[1].x, p.q[1].y, p.q[1].z, p.q[1].w};
+#pragma unroll
+    for (int pl = 0; pl < 3; ++pl) {
+        *reinterpret_cast<u32x4 *>(at + pl * plane) = u32x4{high_halves(x[0], x[1]), high_halves(x[2], x[3]),
+                                                            high_halves(x[4], x[5]), high_halves(x[6], x[7])};
+        if (pl < 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] = __float_as_uint(__uint_as_float(x[i]) - __uint_as_float(x[i] & 0xffff0000u));
+        }
+    }
+}
+
+// Sum of the piece's elements.
+__device__ __forceinline__ float piece_sum(const Piece<uint16_t> &p) {
+    float sum = 0.0f;
+    const u32x4 q = p.q[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += widen((uint16_t)q[i]) + __uint_as_float(q[i] & 0xffff0000u);
+    return sum;
+}
+__device__ __forceinline__ float piece_sum(const Piece<float> &p) {
+    const u32x4 a = p.q[0], b = p.q[1];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += __uint_as_float(a[i]) + __uint_as_float(b[i]);
+    return sum;
+}
+
+// Sum over aligned runs of LANES (4, 8 or 16) lanes, in each of them.
+template <int CTRL>
+__device__ __forceinline__ float plus_moved(float x) {
+    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int LANES>
+__device__ __forceinline__ float run_sum(float x) {
+    x = plus_moved<0xb1>(x);                    // the neighbour
+    x = plus_moved<0x4e>(x);                    // the other pair
+    if (LANES >= 8) x = plus_moved<0x141>(x);   // mirrored in eight: the other quad
+    if (LANES >= 16) x = plus_moved<0x140>(x);  // mirrored in sixteen
+    return x;
+}
+
+// ---- weights ------------------------------------------------------------------------------------------
+// Two bf16 of two bytes 0000uuuu.
+__device__ __forceinline__ uint32_t low_pair(uint32_t bytes) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.0f, false));
+}
+__device__ __forceinline__ uint32_t high_pair(uint32_t bytes) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.0f, true));
+}
+// The eight codes of a dword as an operand.
+__device__ __forceinline__ bf16x8 decode(uint32_t d) {
+    const uint32_t lo = d & 0x0f0f0f0fu, hi = (d >> 4) & 0x0f0f0f0fu;
+    return __builtin_bit_cast(bf16x8, u32x4{low_pair(lo), high_pair(lo), low_pair(hi), high_pair(hi)});
+}
+
+__device__ __forceinline__ bf16x8 lds_operand(const unsigned char *at) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(at));
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 acc) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 acc) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+}
+// Row of the 32 x 32 result of accumulator register i in lane half h; its column is lane % 32.
+__device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// N neighbouring scales and zero points of one row, as loaded.
+template <int N>
+struct Scales {
+    uint32_t s[N];   // wide: each a float32; else two bf16 in each of the first N / 2 (N = 1: one)
+    uint32_t z[(N + 3) / 4];
+};
+template <int N>
+__device__ __forceinline__ Scales<N> load_scales(const Int4 &m, long long idx) {
+    Scales<N> r;
+    if (m.wide) {
+        const uint32_t *p = static_cast<const uint32_t *>(m.scales) + idx;
+        if constexpr (N == 1) r.s[0] = p[0];
+        if constexpr (N == 2) { const u32x2 x = *reinterpret_cast<const u32x2 *>(p); r.s[0] = x.x; r.s[1] = x.y; }
+        if constexpr (N >= 4) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(p + i);
+                r.s[i] = x.x; r.s[i + 1] = x.y; r.s[i + 2] = x.z; r.s[i + 3] = x.w;
+            }
+        }
+    } else {
+        const uint16_t *p = static_cast<const uint16_t *>(m.scales) + idx;
+        if constexpr (N == 1) r.s[0] = p[0];
+        if constexpr (N == 2) r.s[0] = *reinterpret_cast<const uint32_t *>(p);
+        if constexpr (N == 4) { const u32x2 x = *reinterpret_cast<const u32x2 *>(p); r.s[0] = x.x; r.s[1] = x.y; }
+        if constexpr (N == 8) {
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+            r.s[0] = x.x; r.s[1] = x.y; r.s[2] = x.z; r.s[3] = x.w;
+        }
+    }
+    if (m.zeros) {
+        const int8_t *p = m.zeros + idx;
+        if constexpr (N == 1) r.z[0] = (uint8_t)p[0];
+        if constexpr (N == 2) r.z[0] = *reinterpret_cast<const uint16_t *>(p);
+        if constexpr (N >= 4) {
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) r.z[i] = reinterpret_cast<const uint32_t *>(p)[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < (N + 3) / 4; ++i) r.z[i] = 0;
+    }
+    return r;
+}
+template <int N>
+__device__ __forceinline__ float scale_of(const Scales<N> &r, int wide, int i) {
+    const uint32_t narrow = i & 1 ? r.s[i >> 1] & 0xffff0000u : r.s[i >> 1] << 16;
+    return __uint_as_float(wide ? r.s[i] : narrow);
+}
+// (8 + z) / 8, what the sum of -8 x is multiplied with
+template <int N>
+__device__ __forceinline__ float zero_factor(const Scales<N> &r, int i) {
+    return 1.0f + 0.125f * (float)(int)__builtin_amdgcn_sbfe((int)r.z[i >> 2], 8u * (i & 3), 8u);
+}
+
 // Scale and zero point of (row, column): idx = ((row group * tiles + tile) * 16 + row % 16) * groups per tile + group.
 __device__ __forceinline__ float scale_at(const Int4 &m, long long idx) {
     return m.wide ? static_cast<const float *>(m.scales)[idx] : widen(static_cast<const uint16_t *>(m.scales)[idx]);

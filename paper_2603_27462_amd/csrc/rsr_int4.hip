@@ -69,52 +69,149 @@ __global__ __launch_bounds__(256) void k_int4_pack_scales(const float *__restric
     if (zto) zto[gid] = live ? zeros[from] : 0;
 }
 
-// ---- a row of a vector per thread --------------------------------------------------------------------
-template <typename VT>
-__device__ float dot(const Int4 &m, int gpt, int ntiles, const VT *x, int n_in, long long row) {
-    const long long G = row / kDenseRows;
-    const int r = (int)(row % kDenseRows), steps = kInt4Steps / gpt;
-    float sum = 0.0f, part = 0.0f, total = 0.0f;
-    for (int t = 0; t < ntiles; ++t)
-        for (int d = 0; d < kInt4Steps; ++d) {
-            for (int slice = 0; slice < 4; ++slice) {
-                const uint32_t w = m.codes[(G * ntiles + t) * kInt4TileDwords + (d >> 2) * 256 + (16 * slice + r) * 4 + (d & 3)];
-                for (int e = 0; e < 8; ++e) {
-                    const int j = t * kInt4Tile + 32 * d + 8 * slice + e;
-                    if (j >= n_in) break;
-                    const float v = widen(x[j]);
-                    part += (float)((w >> (8 * (e & 3) + 4 * (e >> 2))) & 15u) * v;
-                    total += v;
+// ---- few: up to four vectors ------------------------------------------------------------------------
+// A wave takes 16 rows (of both matrices, if there are two) and a share of the columns; `wk` waves of a workgroup share
+// the columns of a row group and add their partial results at the end, the only place where waves wait for each other.
+// Every wave stages its own columns of v, and the sums of v over the groups, in LDS of its own.  The vectors are the rows of
+// the MFMA: vector q sits in rows 4q.. (float32: its three planes in rows 4q, 4q+1, 4q+2), so that lane 16 q + r of
+// the result holds everything about (vector q, row r), and one MFMA serves all planes.
+// (Two matrices take twice the registers, so at most eight waves.)
+constexpr int few_most_waves(int nm) { return nm == 2 ? 8 : 16; }
+
+template <typename VT, int NV, int GPT>
+struct Few {
+    static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
+    static constexpr int tiles = NV == 1 ? (planes == 3 && GPT == 8 ? 2 : 4) : planes == 3 ? 1 : 2;  // staged at a time
+    static constexpr int cols = tiles * kInt4Tile;
+    static constexpr int pieces = cols / 8;
+    static constexpr int loads = NV * pieces / 64;
+    static constexpr int stride = cols * 2 + 16;  // bytes between slots: an odd number of 16-byte units
+    static constexpr int sums = NV * tiles * GPT;
+    static constexpr int wave_bytes = NV * planes * stride + (sums * 4 + 15) / 16 * 16;
+};
+
+template <typename VT, int NV, int GPT, int NM>
+__global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, Int4 m1, const VT *__restrict__ v, int ntiles, int ngroups,
+                                                  int n_in, int n_out, long long ldv, int nv, int wk_log2, float scale,
+                                                  void *__restrict__ out, int out_bf16, long long ldo, int act,
+                                                  float *__restrict__ pre) {
+    using S = Few<VT, NV, GPT>;
+    constexpr int kSteps = kInt4Steps / GPT, kRun = kInt4Tile / GPT / 8;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w >> wk_log2, wk = w - (wr << wk_log2);
+    const int g = min((int)(blockIdx.x * (waves >> wk_log2)) + wr, ngroups - 1);
+    const int t0 = (int)((long long)ntiles * wk >> wk_log2), t1 = (int)((long long)ntiles * (wk + 1) >> wk_log2);
+    const int m = lane & 15;
+    const Int4 mat[2] = {m0, m1};
+    const uint32_t *code[NM];
+    long long scale_row[NM];
+#pragma unroll
+    for (int k = 0; k < NM; ++k) {
+        code[k] = mat[k].codes + (long long)g * ntiles * kInt4TileDwords + lane * 4;
+        scale_row[k] = ((long long)g * ntiles * kDenseRows + m) * GPT;
+    }
+    unsigned char *mine = smem + w * S::wave_bytes;
+    float *sums = reinterpret_cast<float *>(mine + NV * S::planes * S::stride);
+
+    Piece<VT> p[S::loads];
+    auto request_v = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < S::loads; ++j) {
+            const int i = j * 64 + lane, n = NV == 1 ? 0 : min(i / S::pieces, nv - 1);
+            p[j] = load_piece<VT>(v + n * ldv, t * kInt4Tile + 8 * (i % S::pieces), n_in);
+        }
+    };
+    u32x4 c[NM][S::tiles][2];
+    Scales<GPT> sc[NM][S::tiles];
+    auto request_codes = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < S::tiles; ++i)
+            if (t + i < t1) {
+#pragma unroll
+                for (int k = 0; k < NM; ++k) {
+                    const u32x4 *at = reinterpret_cast<const u32x4 *>(code[k] + (long long)(t + i) * kInt4TileDwords);
+                    c[k][i][0] = __builtin_nontemporal_load(at);
+                    c[k][i][1] = __builtin_nontemporal_load(at + 64);
+                    sc[k][i] = load_scales<GPT>(mat[k], scale_row[k] + (long long)(t + i) * kDenseRows * GPT);
                 }
             }
-            if ((d + 1) % steps == 0) {
-                const long long idx = ((G * ntiles + t) * kDenseRows + r) * gpt + d / steps;
-                const float z = m.zeros ? (float)m.zeros[idx] : 0.0f;
-                sum += scale_at(m, idx) * (part - (8.0f + z) * total);
-                part = total = 0.0f;
+    };
+    const int q = lane >> 4, slot = (NV == 1 ? 0 : m >> 2) * S::planes + (S::planes == 3 ? min(m & 3, 2) : 0);
+    const unsigned char *operand = mine + slot * S::stride + q * 16;
+    const float *sum_of = sums + (NV == 1 ? 0 : q) * S::tiles * GPT;
+    float total[NM] = {};
+    if (t0 < t1) {
+        request_v(t0);
+        request_codes(t0);
+    }
+    for (int t = t0; t < t1; t += S::tiles) {
+#pragma unroll
+        for (int j = 0; j < S::loads; ++j) {
+            const int i = j * 64 + lane;
+            store_piece(mine + (i / S::pieces) * S::planes * S::stride + 16 * (i % S::pieces), S::stride, p[j]);
+            const float x = run_sum<kRun>(piece_sum(p[j]));
+            if (i % kRun == 0) sums[i / kRun] = -8.0f * x;
+        }
+        if (t + S::tiles < t1) request_v(t + S::tiles);
+        // the wave's LDS operations execute in order: no barrier inside a wave
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < S::tiles; ++i) {
+            if (t + i >= t1) break;
+#pragma unroll
+            for (int gr = 0; gr < GPT; ++gr) {
+                f32x4 acc[NM] = {};
+#pragma unroll
+                for (int st = gr * kSteps; st < (gr + 1) * kSteps; ++st) {
+                    const bf16x8 x = lds_operand(operand + i * kInt4Tile * 2 + st * 64);
+#pragma unroll
+                    for (int k = 0; k < NM; ++k) acc[k] = mfma16(x, decode(c[k][i][st >> 2][st & 3]), acc[k]);
+                }
+                const float minus = sum_of[i * GPT + gr];
+#pragma unroll
+                for (int k = 0; k < NM; ++k) {
+                    float part = acc[k].x;
+                    if (S::planes == 3) part += acc[k].y + acc[k].z;
+                    total[k] += scale_of(sc[k][i], mat[k].wide, gr) * (part + minus * zero_factor(sc[k][i], gr));
+                }
             }
         }
-    return sum;
-}
-
-template <typename VT, typename OT>
-__global__ __launch_bounds__(256) void k_int4_rows(Int4 a, Int4 b, int gated, int act, int gpt, int ntiles,
-                                                   const VT *__restrict__ v, int n_in, int n_out, long long ldv,
-                                                   float scale, OT *__restrict__ out, long long ldo, float *__restrict__ pre) {
-    const int row = blockIdx.x * 256 + threadIdx.x;
-    const long long n = blockIdx.y + (long long)blockIdx.z * 32768;
-    if (row >= n_out) return;
-    const float x = dot(a, gpt, ntiles, v + n * ldv, n_in, row);
-    if (!gated) {
-        put(out + n * ldo + row, scale * x);
-        return;
+        if (t + S::tiles < t1) request_codes(t + S::tiles);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
-    const float y = dot(b, gpt, ntiles, v + n * ldv, n_in, row);
-    if (pre) {
-        pre[2 * n * n_out + row] = x;
-        pre[(2 * n + 1) * n_out + row] = y;
+    int group = blockIdx.x * (waves >> wk_log2) + wr;
+    if (wk_log2 > 0) {
+        float *red = reinterpret_cast<float *>(smem + waves * S::wave_bytes);
+#pragma unroll
+        for (int k = 0; k < NM; ++k) red[(w * NM + k) * 64 + lane] = total[k];
+        __syncthreads();
+        if (w >= waves >> wk_log2) return;
+#pragma unroll
+        for (int k = 0; k < NM; ++k) total[k] = 0.0f;
+        for (int i = 0; i < 1 << wk_log2; ++i)
+#pragma unroll
+            for (int k = 0; k < NM; ++k) total[k] += red[(((w << wk_log2) + i) * NM + k) * 64 + lane];
+        group = blockIdx.x * (waves >> wk_log2) + w;
     }
-    put(out + n * ldo + row, activate(act, x) * y);
+    const long long row = (long long)group * kDenseRows + m;
+    if (q >= nv || row >= n_out) return;
+    float result;
+    if (NM == 2) {
+        if (pre) {
+            pre[2 * q * (long long)n_out + row] = total[0];
+            pre[(2 * q + 1) * (long long)n_out + row] = total[1];
+        }
+        result = activate(act, total[0]) * total[NM - 1];
+    } else {
+        result = scale * total[0];
+    }
+    if (out_bf16)
+        put(static_cast<uint16_t *>(out) + q * ldo + row, result);
+    else
+        put(static_cast<float *>(out) + q * ldo + row, result);
 }
 
 }  // namespace
@@ -161,44 +258,99 @@ hipError_t launch_int4_pack(const rsr_handle_s *h, const int8_t *Q, const float 
 
 namespace {
 
-template <typename VT, typename OT>
-hipError_t launch(const rsr_handle_s *a, const rsr_handle_s *b, int act, const void *v, float scale, void *out,
-                  float *pre, int batch, int64_t ldv, int64_t ldo, hipStream_t stream) {
-    const int ntiles = (int)((a->cols + kInt4Tile - 1) / kInt4Tile);
-    const dim3 grid((unsigned)((a->rows + 255) / 256), (unsigned)(batch < 32768 ? batch : 32768));
-    for (int n = 0; n < batch; n += 32768) {
-        const int some = batch - n < 32768 ? batch - n : 32768;
-        hipLaunchKernelGGL((k_int4_rows<VT, OT>), dim3(grid.x, (unsigned)some), dim3(256), 0, stream, int4_of(a),
-                           b ? int4_of(b) : Int4{}, b != nullptr, act, kInt4Tile / a->group, ntiles,
-                           static_cast<const VT *>(v) + n * ldv, (int)a->cols, (int)a->rows, (long long)ldv, scale,
-                           static_cast<OT *>(out) + n * ldo, (long long)ldo, pre ? pre + 2 * n * a->rows : nullptr);
-        if (hipError_t e = hipGetLastError()) return e;
+struct Args {
+    Int4 m[2];
+    const void *v;
+    int ntiles, ngroups, n_in, n_out, batch, device;
+    long long ldv, ldo;
+    float scale;
+    void *out;
+    int out_bf16, act;
+    float *pre;
+    hipStream_t stream;
+};
+
+// Waves that share the columns of a row group: as many as stage all of theirs at once, and more while the chip has fewer
+// than four waves per CU.
+int few_wk_log2(int ntiles, int ngroups, int tiles, int most) {
+    int log2 = 0;
+    while (2 << log2 <= most && (ntiles + tiles - 1) / tiles > 1 << log2) ++log2;
+    while (2 << log2 <= most && 1 << log2 < ntiles && (long long)ngroups << log2 < 1024) ++log2;
+    return log2;
+}
+
+template <typename VT, int NV, int GPT, int NM>
+hipError_t launch_few(const Args &x) {
+    using S = Few<VT, NV, GPT>;
+    static std::atomic<size_t> enabled[kMaxDevices];
+    auto kern = k_int4_few<VT, NV, GPT, NM>;
+    const int wk_log2 = few_wk_log2(x.ntiles, x.ngroups, S::tiles, few_most_waves(NM));
+    int waves = wk_log2 < 2 ? 4 : 1 << wk_log2;
+    const size_t lds = (size_t)waves * (S::wave_bytes + NM * 64 * 4);
+    static_assert(few_most_waves(NM) * (S::wave_bytes + NM * 64 * 4) <= kLdsBytes, "every wave stages columns of its own");
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
+    const int groups = waves >> wk_log2;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((x.ngroups + groups - 1) / groups)), dim3(waves * 64), lds, x.stream, x.m[0],
+                       x.m[1], static_cast<const VT *>(x.v), x.ntiles, x.ngroups, x.n_in, x.n_out, x.ldv, x.batch,
+                       wk_log2, x.scale, x.out, x.out_bf16, x.ldo, x.act, x.pre);
+    return hipGetLastError();
+}
+
+template <typename VT, int GPT, int NM>
+hipError_t launch_any(const Args &x) {
+    if (x.batch == 1) return launch_few<VT, 1, GPT, NM>(x);
+    Args y = x;
+    for (int n = 0; n < x.batch; n += 4) {
+        y.batch = x.batch - n < 4 ? x.batch - n : 4;
+        y.v = static_cast<const VT *>(x.v) + n * x.ldv;
+        y.out = static_cast<unsigned char *>(x.out) + n * x.ldo * (x.out_bf16 ? 2 : 4);
+        if (x.pre) y.pre = x.pre + 2LL * n * x.n_out;
+        if (hipError_t e = launch_few<VT, 4, GPT, NM>(y)) return e;
     }
     return hipSuccess;
 }
 
-template <typename VT>
-hipError_t launch_to(const rsr_handle_s *a, const rsr_handle_s *b, int act, const void *v, float scale, void *out,
-                     int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo, hipStream_t stream) {
-    return out_dtype == RSR_BF16 ? launch<VT, uint16_t>(a, b, act, v, scale, out, pre, batch, ldv, ldo, stream)
-                                 : launch<VT, float>(a, b, act, v, scale, out, pre, batch, ldv, ldo, stream);
+template <typename VT, int NM>
+hipError_t launch_groups(const Args &x, int group) {
+    return group == 32 ? launch_any<VT, 8, NM>(x) : group == 64 ? launch_any<VT, 4, NM>(x) : launch_any<VT, 2, NM>(x);
+}
+
+Args args_of(const rsr_handle_s *a, const rsr_handle_s *b, int act, const void *v, float scale, void *out, int out_dtype,
+             float *pre, int batch, int64_t ldv, int64_t ldo, hipStream_t stream) {
+    Args x = {};
+    x.m[0] = int4_of(a);
+    if (b) x.m[1] = int4_of(b);
+    x.v = v;
+    x.ntiles = (int)((a->cols + kInt4Tile - 1) / kInt4Tile);
+    x.ngroups = (int)row_groups(a->rows);
+    x.n_in = (int)a->cols;
+    x.n_out = (int)a->rows;
+    x.batch = batch;
+    x.device = a->device;
+    x.ldv = ldv;
+    x.ldo = ldo;
+    x.scale = scale;
+    x.out = out;
+    x.out_bf16 = out_dtype == RSR_BF16;
+    x.act = act;
+    x.pre = pre;
+    x.stream = stream;
+    return x;
 }
 
 }  // namespace
 
 hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float scale, void *out, int out_dtype,
                        int batch, int64_t ldv, int64_t ldo, hipStream_t stream) {
-    return v_dtype == RSR_BF16
-               ? launch_to<uint16_t>(h, nullptr, 0, v, scale, out, out_dtype, nullptr, batch, ldv, ldo, stream)
-               : launch_to<float>(h, nullptr, 0, v, scale, out, out_dtype, nullptr, batch, ldv, ldo, stream);
+    const Args x = args_of(h, nullptr, 0, v, scale, out, out_dtype, nullptr, batch, ldv, ldo, stream);
+    return v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group);
 }
 
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,
                              void *out, int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo,
                              hipStream_t stream) {
-    return v_dtype == RSR_BF16
-               ? launch_to<uint16_t>(gate, up, act, v, 1.0f, out, out_dtype, pre, batch, ldv, ldo, stream)
-               : launch_to<float>(gate, up, act, v, 1.0f, out, out_dtype, pre, batch, ldv, ldo, stream);
+    const Args x = args_of(gate, up, act, v, 1.0f, out, out_dtype, pre, batch, ldv, ldo, stream);
+    return v_dtype == RSR_BF16 ? launch_groups<uint16_t, 2>(x, gate->group) : launch_groups<float, 2>(x, gate->group);
 }
 
 }  // namespace rsr
