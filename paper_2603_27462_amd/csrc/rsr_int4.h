@@ -58,14 +58,21 @@ struct Piece {
     u32x4 q[sizeof(VT) / 2];
 };
 
+template <typename VT>
+__device__ __forceinline__ Piece<VT> load_whole_piece(const VT *__restrict__ at) {
+    Piece<VT> p;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(VT) / 2; ++i)
+        p.q[i] = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const unsigned char *>(at) + 16 * i);
+    return p;
+}
+
 // The piece of `row` at column `col`.
 template <typename VT>
 __device__ __forceinline__ Piece<VT> load_piece(const VT *__restrict__ row, int col, int end) {
     Piece<VT> p = {};
     if (col + 8 <= end) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(VT) / 2; ++i)
-            p.q[i] = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const unsigned char *>(row + col) + 16 * i);
+        p = load_whole_piece<VT>(row + col);
     } else if (col < end) {
         uint32_t e[8];
 #pragma unroll

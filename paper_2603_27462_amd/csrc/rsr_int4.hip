@@ -199,7 +199,7 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
     const long long row = (long long)group * kDenseRows + m;
     if (q >= nv || row >= n_out) return;
     float result;
-    if (NM == 2) {
+    if constexpr (NM == 2) {
         if (pre) {
             pre[2 * q * (long long)n_out + row] = total[0];
             pre[(2 * q + 1) * (long long)n_out + row] = total[1];
@@ -212,6 +212,381 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
         put(static_cast<uint16_t *>(out) + q * ldo + row, result);
     else
         put(static_cast<float *>(out) + q * ldo + row, result);
+}
+
+// ---- split: up to 64 vectors ---------------------------------------------------------------------------
+// Eight waves share the columns of G row groups (of each matrix); each stages its own columns of 16 NT vectors, half a tile at
+// a time.  The vectors are the rows of the MFMA: lane l of the result holds row l % 16 of vectors 4 (l / 16) .. + 3.
+constexpr int kSplitWaves = 8;
+
+template <typename VT, int NT, int GPT>
+struct Split {
+    static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
+    static constexpr int vectors = 16 * NT;
+    static constexpr int cols = kInt4Tile / 2;  // staged at a time
+    static constexpr int groups = GPT / 2;      // of them
+    static constexpr int pieces = cols / 8;
+    static constexpr int loads = vectors * pieces / 64;
+    static constexpr int stride = cols * 2 + 16;  // bytes between vectors: an odd number of 16-byte units
+    static constexpr int plane = vectors * stride;
+    static constexpr int wave_bytes = planes * plane + groups * vectors * 4;
+};
+
+template <typename VT, int NT, int GPT, int NM, int G>
+__global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
+    Int4 m0, Int4 m1, const VT *__restrict__ v, int ntiles, int ngroups, int n_in, int n_out, long long ldv, int batch,
+    float scale, void *__restrict__ out, int out_bf16, long long ldo, int act, float *__restrict__ pre) {
+    using S = Split<VT, NT, GPT>;
+    constexpr int kSteps = kInt4Steps / GPT, kRun = kInt4Tile / GPT / 8, kAcc = NM * G * NT * 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int vec0 = blockIdx.y * S::vectors, group0 = blockIdx.x * G;
+    const int halves = (n_in + S::cols - 1) / S::cols;
+    const int h0 = (int)((long long)halves * w / kSplitWaves), h1 = (int)((long long)halves * (w + 1) / kSplitWaves);
+    const Int4 mat[2] = {m0, m1};
+    unsigned char *mine = smem + w * S::wave_bytes;
+    float *sums = reinterpret_cast<float *>(mine + S::planes * S::plane);  // [group][vector]
+
+    const VT *row[S::loads];
+#pragma unroll
+    for (int j = 0; j < S::loads; ++j)
+        row[j] = v + (long long)min(vec0 + (j * 64 + lane) / S::pieces, batch - 1) * ldv;
+    const int piece = lane % S::pieces;
+    const uint32_t *code[NM][G];
+    long long scale_row[NM][G];
+#pragma unroll
+    for (int k = 0; k < NM; ++k)
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const long long rg = min(group0 + g, ngroups - 1);
+            code[k][g] = mat[k].codes + rg * ntiles * kInt4TileDwords + lane * 4;
+            scale_row[k][g] = (rg * ntiles * kDenseRows + (lane & 15)) * GPT;
+        }
+    Piece<VT> p[S::loads];
+    auto request_v = [&](int h) {
+#pragma unroll
+        for (int j = 0; j < S::loads; ++j) p[j] = load_piece<VT>(row[j], h * S::cols + 8 * piece, n_in);
+    };
+    auto request_codes = [&](int h, u32x4 (&c)[NM][G], Scales<S::groups> (&sc)[NM][G]) {
+#pragma unroll
+        for (int k = 0; k < NM; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                c[k][g] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(code[k][g] + (long long)h * 256));
+                sc[k][g] = load_scales<S::groups>(mat[k], scale_row[k][g] + (long long)(h >> 1) * kDenseRows * GPT + (h & 1) * S::groups);
+            }
+    };
+    u32x4 c[NM][G], cn[NM][G];
+    Scales<S::groups> sc[NM][G], scn[NM][G];
+    f32x4 total[NM][G][NT] = {};
+    if (h0 < h1) {
+        request_codes(h0, c, sc);
+        request_v(h0);
+    }
+    for (int h = h0; h < h1; ++h) {
+        request_codes(min(h + 1, h1 - 1), cn, scn);
+#pragma unroll
+        for (int j = 0; j < S::loads; ++j) {
+            const int n = (j * 64 + lane) / S::pieces;
+            store_piece(mine + n * S::stride + 16 * piece, S::plane, p[j]);
+            const float x = run_sum<kRun>(piece_sum(p[j]));
+            if (piece % kRun == 0) sums[piece / kRun * S::vectors + n] = -8.0f * x;
+        }
+        if (h + 1 < h1) request_v(h + 1);
+        // the wave's LDS operations execute in order: no barrier inside a wave
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const unsigned char *operand = mine + (lane & 15) * S::stride + (lane >> 4) * 16;
+#pragma unroll
+        for (int gr = 0; gr < S::groups; ++gr) {
+            f32x4 acc[NM][G][NT] = {};
+#pragma unroll
+            for (int st = gr * kSteps; st < (gr + 1) * kSteps; ++st) {
+                bf16x8 x[NT][S::planes];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int pl = 0; pl < S::planes; ++pl)
+                        x[n][pl] = lds_operand(operand + pl * S::plane + n * 16 * S::stride + st * 64);
+#pragma unroll
+                for (int k = 0; k < NM; ++k)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const bf16x8 y = decode(c[k][g][st]);
+#pragma unroll
+                        for (int pl = 0; pl < S::planes; ++pl)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) acc[k][g][n] = mfma16(x[n][pl], y, acc[k][g][n]);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f32x4 minus = *reinterpret_cast<const f32x4 *>(sums + gr * S::vectors + n * 16 + 4 * (lane >> 4));
+#pragma unroll
+                for (int k = 0; k < NM; ++k)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const float a = scale_of(sc[k][g], mat[k].wide, gr), z = zero_factor(sc[k][g], gr);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) total[k][g][n][i] += a * (acc[k][g][n][i] + minus[i] * z);
+                    }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < NM; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                c[k][g] = cn[k][g];
+                sc[k][g] = scn[k][g];
+            }
+    }
+    __syncthreads();  // the staging areas become the partial results [wave][matrix][group, 16 vectors, register][lane]
+    float *red = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int k = 0; k < NM; ++k)
+#pragma unroll
+        for (int i = 0; i < kAcc / NM; ++i)
+            red[((w * NM + k) * (kAcc / NM) + i) * 64 + lane] = total[k][i / (4 * NT)][i / 4 % NT][i & 3];
+    __syncthreads();
+    for (int i = w; i < kAcc / NM; i += kSplitWaves) {
+        float sum[NM] = {};
+#pragma unroll
+        for (int k = 0; k < NM; ++k)
+#pragma unroll
+            for (int u = 0; u < kSplitWaves; ++u) sum[k] += red[((u * NM + k) * (kAcc / NM) + i) * 64 + lane];
+        const long long r = (long long)(group0 + i / (4 * NT)) * kDenseRows + (lane & 15);
+        const int n = vec0 + i / 4 % NT * 16 + 4 * (lane >> 4) + (i & 3);
+        if (n >= batch || r >= n_out) continue;
+        float result;
+        if constexpr (NM == 2) {
+            if (pre) {
+                pre[2 * n * (long long)n_out + r] = sum[0];
+                pre[(2 * n + 1) * (long long)n_out + r] = sum[1];
+            }
+            result = activate(act, sum[0]) * sum[NM - 1];
+        } else {
+            result = scale * sum[0];
+        }
+        if (out_bf16)
+            put(static_cast<uint16_t *>(out) + n * ldo + r, result);
+        else
+            put(static_cast<float *>(out) + n * ldo + r, result);
+    }
+}
+
+// ---- tile: large batches -----------------------------------------------------------------------------
+// WR x WV waves, each with 64 rows (one matrix) or 32 rows of both, and 32 VB vectors; the vectors are staged in LDS, double
+// buffered, one barrier per stage, and their sums over the groups with them; the codes come straight from memory, every
+// wave those of its own rows.  A stage's group is decoded once into registers for all of the wave's vectors; its sum starts at
+// minus eight times the vector's, and is scaled and added to the result's.
+template <typename VT, int GPT, int WR, int WV, int VB>
+struct Tile {
+    static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
+    static constexpr int threads = 64 * WR * WV;
+    static constexpr int vectors = 32 * WV * VB;
+    static constexpr int cols = sizeof(VT) == 4 ? 64 : 128;  // staged at a time
+    static constexpr int group = kInt4Tile / GPT < cols ? kInt4Tile / GPT : cols;
+    static constexpr int groups = cols / group;
+    static constexpr int scales = cols * GPT / kInt4Tile ? cols * GPT / kInt4Tile : 1;
+    static constexpr int pieces = cols / 8;
+    static constexpr int loads = vectors * pieces / threads;
+    static constexpr int stride = cols * 2 + 16;
+    static constexpr int plane = vectors * stride;
+    static constexpr int buffer = planes * plane + groups * vectors * 4;
+    static constexpr int dwords = cols / 32;  // of a lane and row group
+};
+
+template <typename VT, int GPT, int NM, bool ZEROS, int WR, int WV, int VB>
+__global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
+    Int4 m0, Int4 m1, const VT *__restrict__ v, int ntiles, int ngroups, int n_in, int n_out, long long ldv, int batch,
+    float scale, void *__restrict__ out, int out_bf16, long long ldo, int act, float *__restrict__ pre, int row_tiles,
+    int vec_tiles) {
+    using S = Tile<VT, GPT, WR, WV, VB>;
+    constexpr int kRows = WR * 64 / NM, kRun = S::group / 8;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w % WR, wv = w / WR;
+    // consecutive workgroups go to the eight XCDs in turn: each XCD gets a contiguous run of
+    // tiles, eight row tiles for every vector tile, so that its L2 sees the same vectors again
+    const int all = row_tiles * vec_tiles, per = (all + 7) / 8;
+    const int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || lin >= all) return;
+    const int band = lin / (8 * vec_tiles), in_band = lin - band * 8 * vec_tiles;
+    const int band_rows = min(8, row_tiles - band * 8);
+    const int rt = band * 8 + in_band % band_rows, vec0 = in_band / band_rows * S::vectors;
+    const Int4 mat[2] = {m0, NM == 2 ? m1 : m0};
+
+    // piece j of this thread: of vector mine + j * kApart, a uniform distance further on (no vector there: zeros)
+    constexpr int kApart = S::threads / S::pieces;
+    const int piece = tid % S::pieces, mine = tid / S::pieces;
+    const VT *first = v + (long long)min(vec0 + mine, batch - 1) * ldv + 8 * piece;
+    unsigned char *const to = smem + mine * S::stride + 16 * piece;
+    float *const sum_to = reinterpret_cast<float *>(smem + S::planes * S::plane) + piece / kRun * S::vectors + mine;
+    // row block r: matrix r of two, or the next 32 rows
+    const int row0 = rt * kRows + wr * (64 / NM);
+    const uint32_t *code[2][2];
+    long long scale_row[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int rg = row0 / kDenseRows + (NM == 2 ? 0 : 2 * r);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            code[r][g] = mat[r].codes + (long long)min(rg + g, ngroups - 1) * ntiles * kInt4TileDwords + lane * 4;
+        scale_row[r] = ((long long)min(rg + ((lane >> 4) & 1), ngroups - 1) * ntiles * kDenseRows + (lane & 15)) * GPT;
+    }
+    Piece<VT> p[S::loads];
+    const bool whole = vec0 + S::vectors <= batch;
+    auto request_v = [&](int s) {
+        if (whole && (s + 1) * S::cols <= n_in) {
+#pragma unroll
+            for (int j = 0; j < S::loads; ++j)
+                p[j] = load_whole_piece<VT>(first + j * (kApart * ldv) + s * S::cols);
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::loads; ++j)
+                p[j] = load_piece<VT>(v + (long long)min(vec0 + mine + j * kApart, batch - 1) * ldv, s * S::cols + 8 * piece, n_in);
+        }
+    };
+    auto stage = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < S::loads; ++j) {
+            store_piece(to + buf * S::buffer + j * kApart * S::stride, S::plane, p[j]);
+            const float x = run_sum<kRun>(piece_sum(p[j]));
+            if (piece % kRun == 0) sum_to[buf * (S::buffer / 4) + j * kApart] = -8.0f * x;
+        }
+    };
+    auto request_codes = [&](int s, uint32_t (&c)[2][2][S::dwords], Scales<S::scales> (&sc)[2]) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                if constexpr (S::dwords == 4) {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(code[r][g] + (long long)s * 256);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) c[r][g][d] = x[d];
+                } else {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(code[r][g] + (long long)(s >> 1) * 256 + (s & 1) * 2);
+                    c[r][g][0] = x.x;
+                    c[r][g][1] = x.y;
+                }
+            }
+            constexpr int kPerTile = kInt4Tile / S::cols;
+            sc[r] = load_scales<S::scales>(mat[r], scale_row[r] + (long long)(s / kPerTile) * kDenseRows * GPT +
+                                                       s % kPerTile * S::cols * GPT / kInt4Tile);
+        }
+    };
+    float total[2][VB][16] = {};
+    uint32_t c[2][2][S::dwords], cn[2][2][S::dwords];
+    Scales<S::scales> sc[2], scn[2];
+    const int stages = (n_in + S::cols - 1) / S::cols;
+    request_codes(0, c, sc);
+    request_v(0);
+    stage(0);
+    if (stages > 1) request_v(1);
+    __syncthreads();
+    for (int s = 0; s < stages; ++s) {
+        request_codes(min(s + 1, stages - 1), cn, scn);
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int d = 0; d < S::dwords; ++d) {
+                // lanes below 32: slice 0 (then 1) of both row groups, the others: slice 2 (3)
+                const auto x = __builtin_amdgcn_permlane16_swap(c[r][0][d], c[r][1][d], false, false);
+                c[r][0][d] = x[0];
+                c[r][1][d] = x[1];
+            }
+        const unsigned char *buf = smem + (s & 1) * S::buffer;
+        const float *sums = reinterpret_cast<const float *>(buf + S::planes * S::plane) + wv * 32 * VB + 4 * half;
+        buf += (wv * 32 * VB + (lane & 31)) * S::stride + 32 * half;
+#pragma unroll
+        for (int gr = 0; gr < S::groups; ++gr) {
+            bf16x8 x[2][S::group / 16];
+            float a[2], z[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                for (int ks = 0; ks < S::group / 16; ++ks) x[r][ks] = decode(c[r][ks & 1][gr * (S::group / 32) + ks / 2]);
+                a[r] = scale_of(sc[r], mat[r].wide, S::scales == 1 ? 0 : gr);
+                z[r] = zero_factor(sc[r], S::scales == 1 ? 0 : gr);
+            }
+#pragma unroll
+            for (int n = 0; n < VB; ++n) {
+                f32x16 minus;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 q = *reinterpret_cast<const f32x4 *>(sums + gr * S::vectors + n * 32 + 8 * i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) minus[4 * i + e] = q[e];
+                }
+                f32x16 acc[2] = {minus, minus};
+                if constexpr (ZEROS) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[r][i] *= z[r];
+                }
+#pragma unroll
+                for (int ks = 0; ks < S::group / 16; ++ks)
+#pragma unroll
+                    for (int pl = 0; pl < S::planes; ++pl) {
+                        const bf16x8 o = lds_operand(buf + pl * S::plane + n * 32 * S::stride + gr * S::group * 2 + (ks >> 1) * 64 + (ks & 1) * 16);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) acc[r] = mfma32(o, x[r][ks], acc[r]);
+                    }
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        total[r][n][i] += a[r] * acc[r][i];
+                        // (here, and not behind the branches below: all blocks' sums at once do not fit the registers)
+                        asm volatile("" : "+v"(total[r][n][i]));
+                    }
+            }
+        }
+        // the next stage goes to the other buffer, which nobody reads any more
+        if (s + 1 < stages) stage((s + 1) & 1);
+        if (s + 2 < stages) request_v(s + 2);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int d = 0; d < S::dwords; ++d) c[r][g][d] = cn[r][g][d];
+            sc[r] = scn[r];
+        }
+    }
+    // The codes requested last are not used.  They are waited for here (vmcnt = 0): if one of their
+    // registers comes to hold an address or a result below, every store gets a wait for all that is on its way.
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+#pragma unroll
+    for (int r = 0; r < (NM == 2 ? 1 : 2); ++r) {
+        const int row_out = row0 + r * 32 + (lane & 31);
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const long long n = vec0 + (wv * VB + b) * 32 + acc_row(i, half);
+                if (n >= batch || row_out >= n_out) continue;
+                float result;
+                if constexpr (NM == 2) {
+                    if (pre) {
+                        pre[2 * n * n_out + row_out] = total[0][b][i];
+                        pre[(2 * n + 1) * n_out + row_out] = total[1][b][i];
+                    }
+                    result = activate(act, total[0][b][i]) * total[1][b][i];
+                } else {
+                    result = scale * total[r][b][i];
+                }
+                if (out_bf16)
+                    put(static_cast<uint16_t *>(out) + n * ldo + row_out, result);
+                else
+                    put(static_cast<float *>(out) + n * ldo + row_out, result);
+            }
+    }
 }
 
 }  // namespace
@@ -296,18 +671,56 @@ hipError_t launch_few(const Args &x) {
     return hipGetLastError();
 }
 
+template <typename VT, int NT, int GPT, int NM, int G>
+hipError_t launch_split_rows(const Args &x) {
+    using S = Split<VT, NT, GPT>;
+    static std::atomic<size_t> enabled[kMaxDevices];
+    auto kern = k_int4_split<VT, NT, GPT, NM, G>;
+    constexpr size_t staged = (size_t)kSplitWaves * S::wave_bytes, joined = (size_t)kSplitWaves * NM * G * NT * 4 * 64 * 4;
+    constexpr size_t lds = staged > joined ? staged : joined;
+    static_assert(lds <= (size_t)kLdsBytes, "staging, and then the partial results of all waves");
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((x.ngroups + G - 1) / G), (unsigned)((x.batch + S::vectors - 1) / S::vectors)),
+                       dim3(kSplitWaves * 64), lds, x.stream, x.m[0], x.m[1], static_cast<const VT *>(x.v), x.ntiles, x.ngroups,
+                       x.n_in, x.n_out, x.ldv, x.batch, x.scale, x.out, x.out_bf16, x.ldo, x.act, x.pre);
+    return hipGetLastError();
+}
+
+template <typename VT, int GPT, int NM>
+hipError_t launch_split(const Args &x) {
+    const bool few_rows = x.ngroups < 512;
+    if (x.batch <= 16 || sizeof(VT) == 4)
+        return few_rows ? launch_split_rows<VT, 1, GPT, NM, 1>(x) : launch_split_rows<VT, 1, GPT, NM, 2>(x);
+    return few_rows ? launch_split_rows<VT, sizeof(VT) == 4 ? 1 : 2, GPT, NM, 1>(x)
+                    : launch_split_rows<VT, sizeof(VT) == 4 ? 1 : 2, GPT, NM, 2>(x);
+}
+
+template <typename VT, int GPT, int NM, bool ZEROS, int WR, int WV, int VB>
+hipError_t launch_tile_shape(const Args &x) {
+    using S = Tile<VT, GPT, WR, WV, VB>;
+    static std::atomic<size_t> enabled[kMaxDevices];
+    auto kern = k_int4_tile<VT, GPT, NM, ZEROS, WR, WV, VB>;
+    constexpr size_t lds = 2 * (size_t)S::buffer;
+    static_assert(lds <= (size_t)kLdsBytes, "two stages");
+    if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
+    constexpr int rows = WR * 64 / NM;
+    const int row_tiles = (x.n_out + rows - 1) / rows, vec_tiles = (x.batch + S::vectors - 1) / S::vectors;
+    const int per = (int)(((long long)row_tiles * vec_tiles + 7) / 8);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(per * 8)), dim3(S::threads), lds, x.stream, x.m[0], x.m[1],
+                       static_cast<const VT *>(x.v), x.ntiles, x.ngroups, x.n_in, x.n_out, x.ldv, x.batch, x.scale, x.out,
+                       x.out_bf16, x.ldo, x.act, x.pre, row_tiles, vec_tiles);
+    return hipGetLastError();
+}
+
 template <typename VT, int GPT, int NM>
 hipError_t launch_any(const Args &x) {
     if (x.batch == 1) return launch_few<VT, 1, GPT, NM>(x);
-    Args y = x;
-    for (int n = 0; n < x.batch; n += 4) {
-        y.batch = x.batch - n < 4 ? x.batch - n : 4;
-        y.v = static_cast<const VT *>(x.v) + n * x.ldv;
-        y.out = static_cast<unsigned char *>(x.out) + n * x.ldo * (x.out_bf16 ? 2 : 4);
-        if (x.pre) y.pre = x.pre + 2LL * n * x.n_out;
-        if (hipError_t e = launch_few<VT, 4, GPT, NM>(y)) return e;
-    }
-    return hipSuccess;
+    if (x.batch <= 4) return launch_few<VT, 4, GPT, NM>(x);
+    constexpr int rows = 128 / NM;
+    const long long tiles = (long long)((x.n_out + rows - 1) / rows) * ((x.batch + 127) / 128);
+    if (x.batch <= 32 || tiles < 100) return launch_split<VT, GPT, NM>(x);
+    return x.m[0].zeros || x.m[1].zeros ? launch_tile_shape<VT, GPT, NM, true, 4, 2, 2>(x)
+                                        : launch_tile_shape<VT, GPT, NM, false, 4, 2, 2>(x);
 }
 
 template <typename VT, int NM>
