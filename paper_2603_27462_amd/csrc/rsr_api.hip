@@ -963,7 +963,7 @@ int rsr_int4_matvec(rsr_handle_t h, int transposed, const void *v, int v_dtype, 
     if (batch == 0) return RSR_OK;
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     const hipError_t e =
-        transposed ? rsr::launch_int4_transposed(h, nullptr, v, v_dtype, scale, out, out_dtype, batch, ldv, ldo, s)
+        transposed ? rsr::launch_int4_transposed(h, nullptr, v, v_dtype, false, scale, out, out_dtype, batch, ldv, ldo, s)
                    : rsr::launch_int4(h, v, v_dtype, scale, out, out_dtype, batch, ldv, ldo, s);
     return e == hipSuccess ? RSR_OK : fail(hip_code(e));
 }
@@ -988,7 +988,7 @@ int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, con
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     hipError_t e = rsr::launch_gated_slopes(pre, dout, d_dtype, ldd, act, gate->rows, batch, dpre, s);
     if (e == hipSuccess && dv)
-        e = rsr::launch_int4_transposed(gate, up, dpre, RSR_F32, 1.0f, dv, dv_dtype, batch, 2 * gate->rows, lddv, s);
+        e = rsr::launch_int4_transposed(gate, up, dpre, RSR_F32, true, 1.0f, dv, dv_dtype, batch, 2 * gate->rows, lddv, s);
     return e == hipSuccess ? RSR_OK : fail(hip_code(e));
 }
 
