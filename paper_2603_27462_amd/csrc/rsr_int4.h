@@ -119,9 +119,10 @@ __device__ __forceinline__ void store_piece(unsigned char *at, int plane, const 
 // Sum of the piece's elements.
 __device__ __forceinline__ float piece_sum(const Piece<uint16_t> &p) {
     float sum = 0.0f;
-    const u32x4 q = p.q[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += widen((uint16_t)q[i]) + __uint_as_float(q[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i)
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)p.q[0][i]),
+                                              __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
     return sum;
 }
 __device__ __forceinline__ float piece_sum(const Piece<float> &p) {

@@ -2,6 +2,8 @@
 // matrices of one shape, h = act(Mg x) * (Mu x).
 #include "rsr_int4.h"
 
+#include <type_traits>
+
 namespace rsr {
 
 namespace {
@@ -378,15 +380,17 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
 }
 
 // ---- tile: large batches -----------------------------------------------------------------------------
-// WR x WV waves, each with 64 rows (one matrix) or 32 rows of both, and 32 VB vectors; the vectors are staged in LDS, double
+// Four waves, each with 64 rows (one matrix) or 32 rows of both, and the same 64 vectors; the vectors are staged in LDS, double
 // buffered, one barrier per stage, and their sums over the groups with them; the codes come straight from memory, every
 // wave those of its own rows.  A stage's group is decoded once into registers for all of the wave's vectors; its sum starts at
 // minus eight times the vector's, and is scaled and added to the result's.
-template <typename VT, int GPT, int WR, int WV, int VB>
+constexpr int kTileWaves = 4, kTileVecs = 2;  // 64 rows each; blocks of 32 vectors
+
+template <typename VT, int GPT>
 struct Tile {
     static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
-    static constexpr int threads = 64 * WR * WV;
-    static constexpr int vectors = 32 * WV * VB;
+    static constexpr int threads = 64 * kTileWaves;
+    static constexpr int vectors = 32 * kTileVecs;
     static constexpr int cols = sizeof(VT) == 4 ? 64 : 128;  // staged at a time
     static constexpr int group = kInt4Tile / GPT < cols ? kInt4Tile / GPT : cols;
     static constexpr int groups = cols / group;
@@ -399,16 +403,16 @@ struct Tile {
     static constexpr int dwords = cols / 32;  // of a lane and row group
 };
 
-template <typename VT, int GPT, int NM, bool ZEROS, int WR, int WV, int VB>
-__global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
+template <typename VT, int GPT, int NM, bool ZEROS>
+__global__ __launch_bounds__(64 * kTileWaves, 2) void k_int4_tile(
     Int4 m0, Int4 m1, const VT *__restrict__ v, int ntiles, int ngroups, int n_in, int n_out, long long ldv, int batch,
     float scale, void *__restrict__ out, int out_bf16, long long ldo, int act, float *__restrict__ pre, int row_tiles,
     int vec_tiles) {
-    using S = Tile<VT, GPT, WR, WV, VB>;
-    constexpr int kRows = WR * 64 / NM, kRun = S::group / 8;
+    using S = Tile<VT, GPT>;
+    constexpr int kRows = kTileWaves * 64 / NM, kRun = S::group / 8;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w % WR, wv = w / WR;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     // consecutive workgroups go to the eight XCDs in turn: each XCD gets a contiguous run of
     // tiles, eight row tiles for every vector tile, so that its L2 sees the same vectors again
     const int all = row_tiles * vec_tiles, per = (all + 7) / 8;
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
     unsigned char *const to = smem + mine * S::stride + 16 * piece;
     float *const sum_to = reinterpret_cast<float *>(smem + S::planes * S::plane) + piece / kRun * S::vectors + mine;
     // row block r: matrix r of two, or the next 32 rows
-    const int row0 = rt * kRows + wr * (64 / NM);
+    const int row0 = rt * kRows + w * (64 / NM);
     const uint32_t *code[2][2];
     long long scale_row[2];
 #pragma unroll
@@ -439,8 +443,9 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
     }
     Piece<VT> p[S::loads];
     const bool whole = vec0 + S::vectors <= batch;
+    const int whole_stages = whole ? n_in / S::cols : 0;
     auto request_v = [&](int s) {
-        if (whole && (s + 1) * S::cols <= n_in) {
+        if (s < whole_stages) {
 #pragma unroll
             for (int j = 0; j < S::loads; ++j)
                 p[j] = load_whole_piece<VT>(first + j * (kApart * ldv) + s * S::cols);
@@ -455,7 +460,7 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
         for (int j = 0; j < S::loads; ++j) {
             store_piece(to + buf * S::buffer + j * kApart * S::stride, S::plane, p[j]);
             const float x = run_sum<kRun>(piece_sum(p[j]));
-            if (piece % kRun == 0) sum_to[buf * (S::buffer / 4) + j * kApart] = -8.0f * x;
+            sum_to[buf * (S::buffer / 4) + j * kApart] = -8.0f * x;  // (every lane of the run, the same)
         }
     };
     auto request_codes = [&](int s, uint32_t (&c)[2][2][S::dwords], Scales<S::scales> (&sc)[2]) {
@@ -478,7 +483,7 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
                                                        s % kPerTile * S::cols * GPT / kInt4Tile);
         }
     };
-    float total[2][VB][16] = {};
+    float total[2][kTileVecs][16] = {};
     uint32_t c[2][2][S::dwords], cn[2][2][S::dwords];
     Scales<S::scales> sc[2], scn[2];
     const int stages = (n_in + S::cols - 1) / S::cols;
@@ -487,8 +492,18 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
     stage(0);
     if (stages > 1) request_v(1);
     __syncthreads();
-    for (int s = 0; s < stages; ++s) {
+    auto step = [&](int s, auto steady) {
         request_codes(min(s + 1, stages - 1), cn, scn);
+        // the next stage goes to the other buffer, which nobody reads any more
+        if constexpr (steady) {
+            stage((s + 1) & 1);
+#pragma unroll
+            for (int j = 0; j < S::loads; ++j)
+                p[j] = load_whole_piece<VT>(first + j * (kApart * ldv) + (s + 2) * S::cols);
+        } else {
+            if (s + 1 < stages) stage((s + 1) & 1);
+            if (s + 2 < stages) request_v(s + 2);
+        }
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -499,8 +514,8 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
                 c[r][1][d] = x[1];
             }
         const unsigned char *buf = smem + (s & 1) * S::buffer;
-        const float *sums = reinterpret_cast<const float *>(buf + S::planes * S::plane) + wv * 32 * VB + 4 * half;
-        buf += (wv * 32 * VB + (lane & 31)) * S::stride + 32 * half;
+        const float *sums = reinterpret_cast<const float *>(buf + S::planes * S::plane) + 4 * half;
+        buf += (lane & 31) * S::stride + 32 * half;
 #pragma unroll
         for (int gr = 0; gr < S::groups; ++gr) {
             bf16x8 x[2][S::group / 16];
@@ -513,7 +528,7 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
                 z[r] = zero_factor(sc[r], S::scales == 1 ? 0 : gr);
             }
 #pragma unroll
-            for (int n = 0; n < VB; ++n) {
+            for (int n = 0; n < kTileVecs; ++n) {
                 f32x16 minus;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -546,9 +561,6 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
                     }
             }
         }
-        // the next stage goes to the other buffer, which nobody reads any more
-        if (s + 1 < stages) stage((s + 1) & 1);
-        if (s + 2 < stages) request_v(s + 2);
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -558,7 +570,10 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
                 for (int d = 0; d < S::dwords; ++d) c[r][g][d] = cn[r][g][d];
             sc[r] = scn[r];
         }
-    }
+    };
+    int s = 0;
+    for (; s + 2 < whole_stages; ++s) step(s, std::true_type());
+    for (; s < stages; ++s) step(s, std::false_type());
     // The codes requested last are not used.  They are waited for here (vmcnt = 0): if one of their
     // registers comes to hold an address or a result below, every store gets a wait for all that is on its way.
     __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -566,10 +581,10 @@ __global__ __launch_bounds__(64 * WR * WV, 2) void k_int4_tile(
     for (int r = 0; r < (NM == 2 ? 1 : 2); ++r) {
         const int row_out = row0 + r * 32 + (lane & 31);
 #pragma unroll
-        for (int b = 0; b < VB; ++b)
+        for (int b = 0; b < kTileVecs; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const long long n = vec0 + (wv * VB + b) * 32 + acc_row(i, half);
+                const long long n = vec0 + b * 32 + acc_row(i, half);
                 if (n >= batch || row_out >= n_out) continue;
                 float result;
                 if constexpr (NM == 2) {
@@ -695,15 +710,15 @@ hipError_t launch_split(const Args &x) {
                     : launch_split_rows<VT, sizeof(VT) == 4 ? 1 : 2, GPT, NM, 2>(x);
 }
 
-template <typename VT, int GPT, int NM, bool ZEROS, int WR, int WV, int VB>
+template <typename VT, int GPT, int NM, bool ZEROS>
 hipError_t launch_tile_shape(const Args &x) {
-    using S = Tile<VT, GPT, WR, WV, VB>;
+    using S = Tile<VT, GPT>;
     static std::atomic<size_t> enabled[kMaxDevices];
-    auto kern = k_int4_tile<VT, GPT, NM, ZEROS, WR, WV, VB>;
+    auto kern = k_int4_tile<VT, GPT, NM, ZEROS>;
     constexpr size_t lds = 2 * (size_t)S::buffer;
     static_assert(lds <= (size_t)kLdsBytes, "two stages");
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
-    constexpr int rows = WR * 64 / NM;
+    constexpr int rows = kTileWaves * 64 / NM;
     const int row_tiles = (x.n_out + rows - 1) / rows, vec_tiles = (x.batch + S::vectors - 1) / S::vectors;
     const int per = (int)(((long long)row_tiles * vec_tiles + 7) / 8);
     hipLaunchKernelGGL(kern, dim3((unsigned)(per * 8)), dim3(S::threads), lds, x.stream, x.m[0], x.m[1],
@@ -719,8 +734,7 @@ hipError_t launch_any(const Args &x) {
     constexpr int rows = 128 / NM;
     const long long tiles = (long long)((x.n_out + rows - 1) / rows) * ((x.batch + 127) / 128);
     if (x.batch <= 32 || tiles < 100) return launch_split<VT, GPT, NM>(x);
-    return x.m[0].zeros || x.m[1].zeros ? launch_tile_shape<VT, GPT, NM, true, 4, 2, 2>(x)
-                                        : launch_tile_shape<VT, GPT, NM, false, 4, 2, 2>(x);
+    return x.m[0].zeros || x.m[1].zeros ? launch_tile_shape<VT, GPT, NM, true>(x) : launch_tile_shape<VT, GPT, NM, false>(x);
 }
 
 template <typename VT, int NM>
