@@ -937,7 +937,7 @@ rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int
     if (host[0]) { rc = RSR_EVALUE; goto done; }
     h->wide_scales = host[1] ? 1 : 0;
     own.add(&h->packed, rsr::int4_code_bytes(rows, cols));
-    own.add_bytes(&h->scales, rsr::int4_groups(rows, cols, h->group) * (h->wide_scales ? 4 : 2));
+    own.add_bytes(&h->scales, rsr::int4_groups(rows, cols, h->group) * (h->wide_scales ? 4 : 2) + rsr::kInt4Behind);
     if (zeros) own.add(&h->zeros, rsr::int4_groups(rows, cols, h->group));
     RSR_TRY(own.allocate(h));
     RSR_TRY(rsr::launch_int4_pack(h, Q, scales, zeros, group, flags));

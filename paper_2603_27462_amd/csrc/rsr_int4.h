@@ -7,6 +7,8 @@
 //           one.  Every 32-column step of the matrix cores lies in one group of columns.
 //   scales  [row group][tile][row][groups of the tile], bf16 if every scale is one, else float32
 //   zeros   the same, int8, if there are any
+// Scales are followed by 64 bytes that are read and not used.  The index of a scale is ((row group * tiles + tile) * 16 + row % 16)
+// * groups of a tile + group, less than the bytes of the codes.
 // Groups of columns are 32, 64 or 128 wide here (the widest that divides the caller's): 8, 4 or 2 per tile.
 //
 // A byte 0000uuuu is the 8-bit float (e4m3) u 2^-9, subnormal up to 7, so v_cvt_scalef32_pk_bf16_fp8 with scale 2^9
@@ -174,64 +176,61 @@ __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 acc) {
 // Row of the 32 x 32 result of accumulator register i in lane half h; its column is lane % 32.
 __device__ __forceinline__ int acc_row(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
-// N neighbouring scales and zero points of one row, as loaded.
+// N neighbouring scales and zero points of one row, as loaded: a few words more than bf16 scales have, and some bytes of
+// codes where there are no zero points, rather than a branch, behind which all loads would be waited for.
+typedef uint32_t u32x4_words __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_words __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16_any __attribute__((aligned(1)));
+
 template <int N>
 struct Scales {
-    uint32_t s[N];   // wide: each a float32; else two bf16 in each of the first N / 2 (N = 1: one)
+    uint32_t s[N];   // wide: each a float32; else two bf16 in each of the first N / 2 (N = 1: in either half, odd)
     uint32_t z[(N + 3) / 4];
+    uint32_t odd;
 };
 template <int N>
 __device__ __forceinline__ Scales<N> load_scales(const Int4 &m, long long idx) {
     Scales<N> r;
-    if (m.wide) {
-        const uint32_t *p = static_cast<const uint32_t *>(m.scales) + idx;
-        if constexpr (N == 1) r.s[0] = p[0];
-        if constexpr (N == 2) { const u32x2 x = *reinterpret_cast<const u32x2 *>(p); r.s[0] = x.x; r.s[1] = x.y; }
-        if constexpr (N >= 4) {
-#pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(p + i);
-                r.s[i] = x.x; r.s[i + 1] = x.y; r.s[i + 2] = x.z; r.s[i + 3] = x.w;
-            }
-        }
-    } else {
-        const uint16_t *p = static_cast<const uint16_t *>(m.scales) + idx;
-        if constexpr (N == 1) r.s[0] = p[0];
-        if constexpr (N == 2) r.s[0] = *reinterpret_cast<const uint32_t *>(p);
-        if constexpr (N == 4) { const u32x2 x = *reinterpret_cast<const u32x2 *>(p); r.s[0] = x.x; r.s[1] = x.y; }
-        if constexpr (N == 8) {
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
-            r.s[0] = x.x; r.s[1] = x.y; r.s[2] = x.z; r.s[3] = x.w;
-        }
+    const unsigned char *base = static_cast<const unsigned char *>(m.scales) + (idx << (m.wide ? 2 : 1));
+    const int8_t *z = (m.zeros ? m.zeros : reinterpret_cast<const int8_t *>(m.codes)) + idx;
+    r.odd = 0;
+    if constexpr (N == 1) {
+        r.odd = m.wide ? 0u : (uint32_t)idx & 1u;
+        r.s[0] = *reinterpret_cast<const uint32_t *>(base - 2 * r.odd);
+        r.z[0] = (uint8_t)z[0];
     }
-    if (m.zeros) {
-        const int8_t *p = m.zeros + idx;
-        if constexpr (N == 1) r.z[0] = (uint8_t)p[0];
-        if constexpr (N == 2) r.z[0] = *reinterpret_cast<const uint16_t *>(p);
-        if constexpr (N >= 4) {
+    if constexpr (N == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2_words *>(base);
+        r.s[0] = x.x; r.s[1] = x.y;
+        r.z[0] = *reinterpret_cast<const u16_any *>(z);
+    }
+    if constexpr (N >= 4) {
 #pragma unroll
-            for (int i = 0; i < N / 4; ++i) r.z[i] = reinterpret_cast<const uint32_t *>(p)[i];
+        for (int i = 0; i < N; i += 4) {
+            const u32x4 x = *reinterpret_cast<const u32x4_words *>(base + 4 * i);
+            r.s[i] = x.x; r.s[i + 1] = x.y; r.s[i + 2] = x.z; r.s[i + 3] = x.w;
         }
-    } else {
 #pragma unroll
-        for (int i = 0; i < (N + 3) / 4; ++i) r.z[i] = 0;
+        for (int i = 0; i < N / 4; ++i) r.z[i] = *reinterpret_cast<const u32_any *>(z + 4 * i);
     }
     return r;
 }
 template <int N>
 __device__ __forceinline__ float scale_of(const Scales<N> &r, int wide, int i) {
-    const uint32_t narrow = i & 1 ? r.s[i >> 1] & 0xffff0000u : r.s[i >> 1] << 16;
+    const uint32_t pair = r.s[i >> 1];
+    const uint32_t narrow = N == 1 ? (r.odd ? pair & 0xffff0000u : pair << 16) : i & 1 ? pair & 0xffff0000u : pair << 16;
     return __uint_as_float(wide ? r.s[i] : narrow);
+}
+template <int N>
+__device__ __forceinline__ int zero_of(const Scales<N> &r, const Int4 &m, int i) {
+    const int z = (int)__builtin_amdgcn_sbfe((int)r.z[i >> 2], 8u * (i & 3), 8u);
+    return m.zeros ? z : 0;
 }
 // (8 + z) / 8, what the sum of -8 x is multiplied with
 template <int N>
-__device__ __forceinline__ float zero_factor(const Scales<N> &r, int i) {
-    return 1.0f + 0.125f * (float)(int)__builtin_amdgcn_sbfe((int)r.z[i >> 2], 8u * (i & 3), 8u);
-}
-
-// Scale and zero point of (row, column): idx = ((row group * tiles + tile) * 16 + row % 16) * groups per tile + group.
-__device__ __forceinline__ float scale_at(const Int4 &m, long long idx) {
-    return m.wide ? static_cast<const float *>(m.scales)[idx] : widen(static_cast<const uint16_t *>(m.scales)[idx]);
+__device__ __forceinline__ float zero_factor(const Scales<N> &r, const Int4 &m, int i) {
+    return 1.0f + 0.125f * (float)zero_of(r, m, i);
 }
 
 // ---- activations --------------------------------------------------------------------------------

@@ -176,7 +176,7 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
                 for (int k = 0; k < NM; ++k) {
                     float part = acc[k].x;
                     if (S::planes == 3) part += acc[k].y + acc[k].z;
-                    total[k] += scale_of(sc[k][i], mat[k].wide, gr) * (part + minus * zero_factor(sc[k][i], gr));
+                    total[k] += scale_of(sc[k][i], mat[k].wide, gr) * (part + minus * zero_factor(sc[k][i], mat[k], gr));
                 }
             }
         }
@@ -266,9 +266,14 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
             scale_row[k][g] = (rg * ntiles * kDenseRows + (lane & 15)) * GPT;
         }
     Piece<VT> p[S::loads];
-    auto request_v = [&](int h) {
+    auto request_v = [&](int h, auto steady) {
+        if (steady || (h + 1) * S::cols <= n_in) {
 #pragma unroll
-        for (int j = 0; j < S::loads; ++j) p[j] = load_piece<VT>(row[j], h * S::cols + 8 * piece, n_in);
+            for (int j = 0; j < S::loads; ++j) p[j] = load_whole_piece<VT>(row[j] + h * S::cols + 8 * piece);
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::loads; ++j) p[j] = load_piece<VT>(row[j], h * S::cols + 8 * piece, n_in);
+        }
     };
     auto request_codes = [&](int h, u32x4 (&c)[NM][G], Scales<S::groups> (&sc)[NM][G]) {
 #pragma unroll
@@ -279,15 +284,15 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
                 sc[k][g] = load_scales<S::groups>(mat[k], scale_row[k][g] + (long long)(h >> 1) * kDenseRows * GPT + (h & 1) * S::groups);
             }
     };
-    u32x4 c[NM][G], cn[NM][G];
-    Scales<S::groups> sc[NM][G], scn[NM][G];
-    f32x4 total[NM][G][NT] = {};
-    if (h0 < h1) {
-        request_codes(h0, c, sc);
-        request_v(h0);
-    }
-    for (int h = h0; h < h1; ++h) {
-        request_codes(min(h + 1, h1 - 1), cn, scn);
+    constexpr int kAhead = NM * G * NT <= 2 ? 4 : NM * G * NT <= 4 ? 2 : 1;  // half tiles whose codes are on their way
+    u32x4 codes[kAhead][NM][G];
+    Scales<S::groups> scales[kAhead][NM][G];
+    float total[NM][G][NT][4] = {};
+    if (h0 < h1) request_v(h0, std::false_type());
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d)
+        if (h0 + d < h1) request_codes(h0 + d, codes[d], scales[d]);
+    auto step = [&](int h, u32x4 (&c)[NM][G], Scales<S::groups> (&sc)[NM][G], auto steady) {
 #pragma unroll
         for (int j = 0; j < S::loads; ++j) {
             const int n = (j * 64 + lane) / S::pieces;
@@ -295,7 +300,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
             const float x = run_sum<kRun>(piece_sum(p[j]));
             if (piece % kRun == 0) sums[piece / kRun * S::vectors + n] = -8.0f * x;
         }
-        if (h + 1 < h1) request_v(h + 1);
+        if (steady || h + 1 < h1) request_v(h + 1, steady);
         // the wave's LDS operations execute in order: no barrier inside a wave
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -329,21 +334,29 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
                 for (int k = 0; k < NM; ++k)
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        const float a = scale_of(sc[k][g], mat[k].wide, gr), z = zero_factor(sc[k][g], gr);
+                        const float a = scale_of(sc[k][g], mat[k].wide, gr), z = zero_factor(sc[k][g], mat[k], gr);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) total[k][g][n][i] += a * (acc[k][g][n][i] + minus[i] * z);
+                        for (int i = 0; i < 4; ++i) {
+                            total[k][g][n][i] += a * (acc[k][g][n][i] + minus[i] * z);
+                            asm volatile("" : "+v"(total[k][g][n][i]));  // (here: see k_int4_tile)
+                        }
                     }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        if (steady || h + kAhead < h1) request_codes(h + kAhead, c, sc);
+    };
+    int h = h0;
+    // (the last half tile may not be whole)
+    for (const int end = min(h1, n_in / S::cols) - 2 * kAhead + 1; h < end; h += kAhead) {
 #pragma unroll
-        for (int k = 0; k < NM; ++k)
+        for (int d = 0; d < kAhead; ++d) step(h + d, codes[d], scales[d], std::true_type());
+    }
+    for (; h < h1; h += kAhead) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                c[k][g] = cn[k][g];
-                sc[k][g] = scn[k][g];
-            }
+        for (int d = 0; d < kAhead; ++d)
+            if (h + d < h1) step(h + d, codes[d], scales[d], std::false_type());
     }
     __syncthreads();  // the staging areas become the partial results [wave][matrix][group, 16 vectors, register][lane]
     float *red = reinterpret_cast<float *>(smem);
@@ -525,7 +538,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void k_int4_tile(
 #pragma unroll
                 for (int ks = 0; ks < S::group / 16; ++ks) x[r][ks] = decode(c[r][ks & 1][gr * (S::group / 32) + ks / 2]);
                 a[r] = scale_of(sc[r], mat[r].wide, S::scales == 1 ? 0 : gr);
-                z[r] = zero_factor(sc[r], S::scales == 1 ? 0 : gr);
+                z[r] = zero_factor(sc[r], mat[r], S::scales == 1 ? 0 : gr);
             }
 #pragma unroll
             for (int n = 0; n < kTileVecs; ++n) {

@@ -2,22 +2,66 @@
 // gated block's activation.
 #include "rsr_int4.h"
 
+#include <type_traits>
+
 namespace rsr {
 
 namespace {
 
-// (da, db) from (a, b) and dh, one thread per element; dpre may be pre.
+// (da, db) from (a, b) and dh, four elements of a vector per thread; dpre may be pre.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
 template <typename VT>
 __global__ __launch_bounds__(256) void k_gated_slopes(const float *pre, const VT *__restrict__ dh, long long ldd, int act,
-                                                      int rows, long long count, float *dpre) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    const long long n = i / rows, r = i - n * rows, at = 2 * n * rows + r;
-    const float a = pre[at], b = pre[at + rows], d = widen(dh[n * ldd + r]);
-    float slope;
-    const float f = activate(act, a, &slope);
-    dpre[at] = d * b * slope;
-    dpre[at + rows] = d * f;
+                                                      int rows, float *dpre) {
+    const int r = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;
+    if (r >= rows) return;
+    const long long n = blockIdx.y, at = 2 * n * rows + r;
+    const VT *from = dh + n * ldd + r;
+    float a[4], b[4], d[4];
+    const int live = min(4, rows - r);
+    if (live == 4) {
+        const f32x4_any x = *reinterpret_cast<const f32x4_any *>(pre + at), y = *reinterpret_cast<const f32x4_any *>(pre + at + rows);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = x[i];
+            b[i] = y[i];
+        }
+        if constexpr (sizeof(VT) == 4) {
+            const f32x4_any z = *reinterpret_cast<const f32x4_any *>(from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = z[i];
+        } else {
+            const u16x4_any z = *reinterpret_cast<const u16x4_any *>(from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d[i] = widen((uint16_t)z[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = i < live ? pre[at + i] : 0.0f;
+            b[i] = i < live ? pre[at + rows + i] : 0.0f;
+            d[i] = i < live ? widen(from[i]) : 0.0f;
+        }
+    }
+    f32x4_any da, db;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float slope;
+        const float f = activate(act, a[i], &slope);
+        da[i] = d[i] * b[i] * slope;
+        db[i] = d[i] * f;
+    }
+    if (live == 4) {
+        *reinterpret_cast<f32x4_any *>(dpre + at) = da;
+        *reinterpret_cast<f32x4_any *>(dpre + at + rows) = db;
+    } else {
+        for (int i = 0; i < live; ++i) {
+            dpre[at + i] = da[i];
+            dpre[at + rows + i] = db[i];
+        }
+    }
 }
 
 // ---- the transposed product ----------------------------------------------------------------------------
@@ -58,11 +102,11 @@ __device__ __forceinline__ void widen_piece(const Piece<float> &p, float (&x)[8]
     for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(p.q[i >> 2][i & 3]);
 }
 
-// Eight rows of dy, scaled, to LDS; returns t + their sum times (8 + z), of what was written.  zeros: 8 + z in bf16, in the order
-// that the rows are written in.
+// Eight rows of dy, scaled, to LDS; adds their sum times (8 + z), of what was written, to t: of three planes that of the top
+// one to t[0], of the others to t[1].  zeros: 8 + z in bf16, in the order that the rows are written in.
 template <int PLANES>
-__device__ __forceinline__ float stage_scaled(const float (&x)[8], const float (&scale)[8], u32x4 zeros, unsigned char *at,
-                                              int plane, float t) {
+__device__ __forceinline__ void stage_scaled(const float (&x)[8], const float (&scale)[8], u32x4 zeros, unsigned char *at,
+                                             int plane, float (&t)[PLANES == 3 ? 2 : 1]) {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = x[i] * scale[i];
@@ -71,27 +115,30 @@ __device__ __forceinline__ float stage_scaled(const float (&x)[8], const float (
         *reinterpret_cast<u32x4 *>(at) = w;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            t = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w[i]), __builtin_bit_cast(bf16x2, (uint32_t)zeros[i]), t, false);
+            t[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w[i]),
+                                                   __builtin_bit_cast(bf16x2, (uint32_t)zeros[i]), t[0], false);
     } else {
         uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int from = i < 4 ? 2 * i : 2 * i - 7;
-            b[i] = __float_as_uint(y[from]);
-            t += y[from] * __uint_as_float(i & 1 ? zeros[i >> 1] & 0xffff0000u : zeros[i >> 1] << 16);
-        }
+        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(y[i < 4 ? 2 * i : 2 * i - 7]);
 #pragma unroll
         for (int pl = 0; pl < 3; ++pl) {
             *reinterpret_cast<u32x4 *>(at + pl * plane) =
                 u32x4{high_halves(b[0], b[1]), high_halves(b[2], b[3]), high_halves(b[4], b[5]), high_halves(b[6], b[7])};
             if (pl < 2) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    b[i] = __float_as_uint(__uint_as_float(b[i]) - __uint_as_float(b[i] & 0xffff0000u));
+                for (int i = 0; i < 8; ++i) {
+                    const float z = __uint_as_float(i & 1 ? zeros[i >> 1] & 0xffff0000u : zeros[i >> 1] << 16);
+                    const float top = __uint_as_float(b[i] & 0xffff0000u), rest = __uint_as_float(b[i]) - top;
+                    if (pl == 0) {
+                        t[0] += top * z;
+                        t[PLANES == 3 ? 1 : 0] += rest * z;
+                    }
+                    b[i] = __float_as_uint(rest);
+                }
             }
         }
     }
-    return t;
 }
 
 // Scales of a run of rows in LDS: float32 [group][row], and 8 + z in bf16 [group][row in the order of the operands].
@@ -102,13 +149,16 @@ __device__ __forceinline__ void put_scale(float *scales, uint16_t *zeros, int at
 }
 
 // ---- tile: 128 columns --------------------------------------------------------------------------------
-// Two waves beside each other in columns, 64 each, and two in vectors, 32 VB each.  A stage is ROWS rows of one matrix: dy scaled
-// for each of the NG groups of the 128 columns, and the codes.  One barrier per stage.
-template <typename VT, int PLANES, int NG, int VB, int ROWS>
+// Two waves beside each other in columns, 64 each, and two in vectors, 32 VB each; KW = 2: two such sets, one multiplies the
+// first eight rows of every row group and one the others, and they add up at the end.  A stage is ROWS rows of one matrix: dy
+// scaled for each of the NG groups of the 128 columns, and the codes.  One barrier per stage.
+// Three planes: the top one has sums of its own, whose products have few bits and add up almost exactly.
+template <typename VT, int PLANES, int NG, int VB, int ROWS, int KW>
 struct BackTile {
+    static constexpr int threads = 256 * KW;
     static constexpr int vectors = 64 * VB;
     static constexpr int pieces = ROWS / 8;
-    static constexpr int loads = vectors * pieces / 256;
+    static constexpr int loads = vectors * pieces / threads;
     static constexpr int stride = ROWS * 2 + 16;  // bytes between vectors: an odd number of 16-byte units
     static constexpr int plane = vectors * stride;
     static constexpr int copy = PLANES * plane;   // of a group
@@ -116,18 +166,22 @@ struct BackTile {
     static constexpr int codes = NG * copy;
     static constexpr int buffer = codes + row_groups * kCodeGroup;
     static constexpr int table = NG * ROWS * 6;   // scales and zero points
-    static constexpr int bytes = 2 * buffer + 2 * table;
+    static constexpr int sums = PLANES == 3 ? 2 : 1;
+    static constexpr int staged = 2 * buffer + 2 * table;
+    static constexpr int joined = KW == 2 ? 4 * 32 * 64 * 4 : 0;
+    static constexpr int bytes = staged > joined ? staged : joined;
 };
 
-template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS>
-__global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int both, int gpt, const VT *__restrict__ dy,
-                                                          int ntiles, int n_rows, int n_cols, long long ldv, int batch,
-                                                          float scale, OT *__restrict__ out, long long ldo, int col_tiles,
-                                                          int vec_tiles) {
-    using S = BackTile<VT, PLANES, NG, VB, ROWS>;
+template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS, int KW>
+__global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int both, int gpt,
+                                                               const VT *__restrict__ dy, int ntiles, int n_rows,
+                                                               int n_cols, long long ldv, int batch, float scale,
+                                                               OT *__restrict__ out, long long ldo, int col_tiles,
+                                                               int vec_tiles) {
+    using S = BackTile<VT, PLANES, NG, VB, ROWS, KW>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wc = w & 1, wv = w >> 1;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wc = w & 1, wv = (w >> 1) & 1, kw = w >> 2;
     // each XCD gets a contiguous run of tiles, eight column tiles for every vector tile
     const int all = col_tiles * vec_tiles, per = (all + 7) / 8;
     const int lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -139,66 +193,67 @@ __global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int
     const int ngroups = (n_rows + kDenseRows - 1) / kDenseRows;
     const int stages1 = (n_rows + ROWS - 1) / ROWS, stages = both ? 2 * stages1 : stages1;
 
-    constexpr int kApart = 256 / S::pieces;
+    constexpr int kApart = S::threads / S::pieces;
     const int piece = tid % S::pieces, mine = tid / S::pieces;
     const VT *first = dy + (long long)min(vec0 + mine, batch - 1) * ldv + 8 * piece;
     const bool whole = vec0 + S::vectors <= batch;
+    const int whole_stages = whole ? n_rows / ROWS : 0;  // of a matrix
     Piece<VT> p[S::loads];
-    auto request_v = [&](int s) {
-        const int k = s >= stages1, row = (s - k * stages1) * ROWS;
-        if (whole && row + ROWS <= n_rows) {
+    auto request_whole = [&](int k, int s) {
 #pragma unroll
-            for (int j = 0; j < S::loads; ++j)
-                p[j] = load_whole_piece<VT>(first + j * (kApart * ldv) + (long long)k * n_rows + row);
+        for (int j = 0; j < S::loads; ++j)
+            p[j] = load_whole_piece<VT>(first + j * (kApart * ldv) + (long long)k * n_rows + s * ROWS);
+    };
+    auto request_v = [&](int s) {
+        const int k = s >= stages1, sk = s - k * stages1;
+        if (sk < whole_stages) {
+            request_whole(k, sk);
         } else {
 #pragma unroll
             for (int j = 0; j < S::loads; ++j)
                 p[j] = load_piece<VT>(dy + (long long)min(vec0 + mine + j * kApart, batch - 1) * ldv + (long long)k * n_rows,
-                                      row + 8 * piece, n_rows);
+                                      sk * ROWS + 8 * piece, n_rows);
         }
     };
-    // codes: a thread per (row group, lane)
+    // codes: a thread per (row group, lane); a thread per (group, row) for the scales
     u32x4 c;
-    const bool has_codes = tid < S::row_groups * 64;
+    constexpr int kScales = (NG * ROWS + S::threads - 1) / S::threads;
+    Scales<1> sv[kScales];
+    const int code_group = (tid >> 6) % S::row_groups;  // (further threads: the same again)
     auto request_codes = [&](int s) {
-        if (!has_codes) return;
         const int k = s >= stages1;
-        const long long rg = min((s - k * stages1) * S::row_groups + (tid >> 6), ngroups - 1);
+        const long long rg = min((s - k * stages1) * S::row_groups + code_group, ngroups - 1);
         c = *reinterpret_cast<const u32x4 *>((k ? m1.codes : m0.codes) + ((rg * ntiles + tile) * 2 + part) * 256 + lane * 4);
     };
     auto put_codes = [&](int buf) {
-        if (!has_codes) return;
-        uint32_t *to = reinterpret_cast<uint32_t *>(smem + buf * S::buffer + S::codes + (tid >> 6) * kCodeGroup + (lane & 15) * kCodeRow) + (lane >> 4);
+        uint32_t *to = reinterpret_cast<uint32_t *>(smem + buf * S::buffer + S::codes + code_group * kCodeGroup + (lane & 15) * kCodeRow) + (lane >> 4);
 #pragma unroll
         for (int d = 0; d < 4; ++d) to[4 * d] = c[d];
     };
-    // scales: a thread per (group, row)
-    constexpr int kScales = (NG * ROWS + 255) / 256;
-    float sv[kScales];
-    int zv[kScales];
+    auto pick = [&](int k) {
+        return Int4{k ? m1.codes : m0.codes, k ? m1.scales : m0.scales, k ? m1.zeros : m0.zeros, k ? m1.wide : m0.wide};
+    };
     auto request_scales = [&](int s) {
         const int k = s >= stages1;
-        const Int4 &m = k ? m1 : m0;
+        const Int4 m = pick(k);
 #pragma unroll
         for (int j = 0; j < kScales; ++j) {
-            const int i = j * 256 + tid, r = (s - k * stages1) * ROWS + i % ROWS, g = i / ROWS;
-            if (i >= NG * ROWS) break;
+            const int i = (j * S::threads + tid) % (NG * ROWS), r = (s - k * stages1) * ROWS + i % ROWS, g = i / ROWS;
             const long long rg = min(r / kDenseRows, ngroups - 1);
             const long long idx = ((rg * ntiles + tile) * kDenseRows + r % kDenseRows) * gpt + part * NG + g;
-            sv[j] = scale_at(m, idx);
-            zv[j] = m.zeros ? m.zeros[idx] : 0;
+            sv[j] = load_scales<1>(m, idx);
         }
     };
     float *const table = reinterpret_cast<float *>(smem + 2 * S::buffer);
-    auto put_scales = [&](int buf) {
+    auto put_scales = [&](int s, int buf) {
+        const Int4 m = pick(s >= stages1);
         float *to = table + buf * (S::table / 4);
 #pragma unroll
-        for (int j = 0; j < kScales; ++j) {
-            const int i = j * 256 + tid;
-            if (i < NG * ROWS) put_scale(to, reinterpret_cast<uint16_t *>(to + NG * ROWS), i, sv[j], zv[j]);
-        }
+        for (int j = 0; j < kScales; ++j)
+            put_scale(to, reinterpret_cast<uint16_t *>(to + NG * ROWS), (j * S::threads + tid) % (NG * ROWS),
+                      scale_of(sv[j], m.wide, 0), zero_of(sv[j], m, 0));
     };
-    float minus[NG][S::loads] = {};
+    float minus[NG][S::loads][S::sums] = {};
     auto stage = [&](int buf) {
         unsigned char *to = smem + buf * S::buffer + mine * S::stride + 16 * piece;
         const float *from = table + buf * (S::table / 4);
@@ -215,16 +270,16 @@ __global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int
             for (int j = 0; j < S::loads; ++j) {
                 float x[8];
                 widen_piece(p[j], x);
-                minus[g][j] = stage_scaled<PLANES>(x, sc, z, to + g * S::copy + j * kApart * S::stride, S::plane, minus[g][j]);
+                stage_scaled<PLANES>(x, sc, z, to + g * S::copy + j * kApart * S::stride, S::plane, minus[g][j]);
             }
         }
     };
-    f32x16 acc[2][VB] = {};
+    f32x16 acc[S::sums][2][VB] = {};
     request_scales(0);
-    put_scales(0);
+    put_scales(0, 0);
     if (stages > 1) {
         request_scales(1);
-        put_scales(1);
+        put_scales(1, 1);
     }
     request_codes(0);
     request_v(0);
@@ -237,7 +292,21 @@ __global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int
     }
     if (stages > 2) request_scales(2);
     __syncthreads();
-    for (int s = 0; s < stages; ++s) {
+    auto step = [&](int s, auto steady) {
+        // the next stage goes to the other buffer, which nobody reads any more
+        if (steady || s + 1 < stages) {
+            put_codes((s + 1) & 1);
+            stage((s + 1) & 1);
+        }
+        if (steady || s + 2 < stages) {
+            put_scales(s + 2, s & 1);
+            request_codes(s + 2);
+            if constexpr (steady)
+                request_whole(s + 2 >= stages1, s + 2 - (s + 2 >= stages1) * stages1);
+            else
+                request_v(s + 2);
+        }
+        request_scales(min(s + 3, stages - 1));
         const unsigned char *buf = smem + (s & 1) * S::buffer;
         const unsigned char *operand = buf + (wv * 32 * VB + (lane & 31)) * S::stride + 32 * half;
         // lanes 0..15 and 16..31: the halves of a 32-column step, lanes from 32 on: the second row group
@@ -248,47 +317,73 @@ __global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int
 #pragma unroll
             for (int r = 0; r < 2; ++r) y[r] = turned(code + q * 2 * kCodeGroup + 16 * r);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int mm = 0; mm < 2 / KW; ++mm) {
                 bf16x8 x[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) x[r] = decode((uint32_t)y[r][m]);
+                for (int r = 0; r < 2; ++r) x[r] = decode((uint32_t)(KW == 1 ? y[r][mm] : kw ? y[r].y : y[r].x));
+                const unsigned char *at_m = operand + 64 * q + 16 * (KW == 1 ? mm : kw);
 #pragma unroll
                 for (int n = 0; n < VB; ++n)
 #pragma unroll
                     for (int pl = 0; pl < PLANES; ++pl) {
-                        const unsigned char *at = operand + pl * S::plane + n * 32 * S::stride + 64 * q + 16 * m;
+                        const unsigned char *at = at_m + pl * S::plane + n * 32 * S::stride;
                         bf16x8 o[2];
                         // (groups of this wave's two 32-column steps: one of all 128 columns, one per 64, one per 32)
                         o[0] = lds_operand(at + (NG == 1 ? 0 : NG == 2 ? wc : 2 * wc) * S::copy);
                         o[1] = NG == 4 ? lds_operand(at + (2 * wc + 1) * S::copy) : o[0];
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) acc[r][n] = mfma32(o[r], x[r], acc[r][n]);
+                        for (int r = 0; r < 2; ++r) {
+                            f32x16 &to = acc[pl ? S::sums - 1 : 0][r][n];
+                            to = mfma32(o[r], x[r], to);
+                        }
                     }
             }
         }
-        // the next stage goes to the other buffer, which nobody reads any more
-        if (s + 1 < stages) {
-            put_codes((s + 1) & 1);
-            stage((s + 1) & 1);
-        }
-        if (s + 2 < stages) {
-            put_scales(s & 1);
-            request_codes(s + 2);
-            request_v(s + 2);
-        }
-        if (s + 3 < stages) request_scales(s + 3);
         __syncthreads();
+    };
+    int s = 0;
+    while (s < stages) {
+        const int end = s < stages1 ? 0 : stages1, far = end + whole_stages - 2;  // steps whose next but one is whole and of the same matrix
+        for (; s < far; ++s) step(s, std::true_type());
+        for (const int last = end + stages1; s < last; ++s) step(s, std::false_type());
     }
-    // what is taken off, per group and vector (the last barrier is behind every read of the buffers)
+    // (the scales requested last are not used; waited for here, so that no store below has to)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    if constexpr (S::sums == 2) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int n = 0; n < VB; ++n) acc[0][r][n] += acc[1][r][n];
+    }
+    if constexpr (KW == 2) {
+        // the second set hands over its sums, 32 registers at a time (the last barrier is behind every read of the buffers)
+        float *red = reinterpret_cast<float *>(smem) + (w & 3) * 2048 + lane;
+#pragma unroll
+        for (int n = 0; n < VB; ++n) {
+            if (kw == 1) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) red[i * 64] = acc[0][i >> 4][n][i & 15];
+            }
+            __syncthreads();
+            if (kw == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) acc[0][i >> 4][n][i & 15] += red[i * 64];
+            }
+            __syncthreads();
+        }
+    }
+    // what is taken off, per group and vector
     float *off = reinterpret_cast<float *>(smem);
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int j = 0; j < S::loads; ++j) {
-            const float t = run_sum<S::pieces>(minus[g][j]);
+            float t = run_sum<S::pieces>(minus[g][j][0]);
+            if (S::sums == 2) t += run_sum<S::pieces>(minus[g][j][S::sums - 1]);
             if (piece == 0) off[g * S::vectors + mine + j * kApart] = t;
         }
     __syncthreads();
+    if (kw == 1) return;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int col = ct * 128 + wc * 64 + r * 32 + turned_column(lane & 31);
@@ -298,7 +393,8 @@ __global__ __launch_bounds__(256, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int v = (wv * VB + n) * 32 + acc_row(i, half);
-                if (vec0 + v < batch && col < n_cols) put(out + (long long)(vec0 + v) * ldo + col, scale * (acc[r][n][i] - o[v]));
+                if (vec0 + v < batch && col < n_cols)
+                    put(out + (long long)(vec0 + v) * ldo + col, scale * (acc[0][r][n][i] - o[v]));
             }
     }
 }
@@ -325,6 +421,7 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
                                                                        int n_cols, long long ldv, int batch, float scale,
                                                                        OT *__restrict__ out, long long ldo, int col_tiles) {
     using S = BackSplit<PLANES, NG>;
+    constexpr int kAhead = sizeof(VT) == 4 ? 2 : 4;  // steps whose loads are on their way
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -341,42 +438,54 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
     uint16_t *table_z = reinterpret_cast<uint16_t *>(table + NG * S::rows);
 
     const int piece = lane & 3;  // eight rows, of vectors lane / 4 and 16 further on
-    Piece<VT> p[2];
-    u32x2 c[2];                  // of two row groups
-    float sv;                    // scale of row lane % 32, group lane / 32
-    int zv;
-    auto request = [&](int s) {
+    Piece<VT> p[kAhead][2];
+    u32x2 c[kAhead][2];          // of two row groups
+    Scales<1> sv[kAhead];        // of row lane % 32, group lane / 32
+    auto pick = [&](int k) {
+        return Int4{k ? m1.codes : m0.codes, k ? m1.scales : m0.scales, k ? m1.zeros : m0.zeros, k ? m1.wide : m0.wide};
+    };
+    const VT *first[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) first[j] = dy + (long long)min(vec0 + 16 * j + (lane >> 2), batch - 1) * ldv;
+    auto request = [&](int slot, int s, auto steady) {
         const int k = s >= steps1, row = (s - k * steps1) * S::rows;
-        const Int4 &m = k ? m1 : m0;
+        const Int4 m = pick(k);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const long long rg = min(row / kDenseRows + j, ngroups - 1);
-            c[j] = *reinterpret_cast<const u32x2 *>(m.codes + ((rg * ntiles + tile) * 2 + (quarter >> 1)) * 256 + lane * 4 + (quarter & 1) * 2);
+            c[slot][j] = *reinterpret_cast<const u32x2 *>(m.codes + ((rg * ntiles + tile) * 2 + (quarter >> 1)) * 256 + lane * 4 + (quarter & 1) * 2);
         }
         const long long rg = min((row + (lane & 31)) / kDenseRows, ngroups - 1);
         const long long idx = ((rg * ntiles + tile) * kDenseRows + (lane & 15)) * gpt + (NG == 2 ? 2 * quarter + half : quarter * gpt / 4);
-        sv = scale_at(m, idx);
-        zv = m.zeros ? m.zeros[idx] : 0;
+        sv[slot] = load_scales<1>(m, idx);
+        if (steady || row + S::rows <= n_rows) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            p[j] = load_piece<VT>(dy + (long long)min(vec0 + 16 * j + (lane >> 2), batch - 1) * ldv + (long long)k * n_rows,
-                                  row + 8 * piece, n_rows);
+            for (int j = 0; j < 2; ++j) p[slot][j] = load_whole_piece<VT>(first[j] + (long long)k * n_rows + row + 8 * piece);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) p[slot][j] = load_piece<VT>(first[j] + (long long)k * n_rows, row + 8 * piece, n_rows);
+        }
     };
-    f32x16 acc[2] = {};
-    float minus[NG][2] = {};
-    if (s0 < s1) request(s0);
-    for (int s = s0; s < s1; ++s) {
-        if (NG == 2 || half == 0) put_scale(table, table_z, lane, sv, zv);
+    constexpr int kSums = PLANES == 3 ? 2 : 1;  // the top plane, and the others
+    f32x16 acc[kSums][2] = {};
+    float minus[NG][2][kSums] = {};
+#pragma unroll
+    for (int d = 0; d < kAhead; ++d)
+        if (s0 + d < s1) request(d, s0 + d, std::false_type());
+    auto step = [&](int d, int s, auto steady) {
+        const Int4 m = pick(s >= steps1);
+        // (one group: the upper half of the lanes writes the same again)
+        put_scale(table, table_z, NG == 2 ? lane : lane & 31, scale_of(sv[d], m.wide, 0), zero_of(sv[d], m, 0));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             uint32_t *to = reinterpret_cast<uint32_t *>(mine + S::codes + (j * kDenseRows + (lane & 15)) * S::row_bytes) + (lane >> 4);
-            to[0] = c[j].x;
-            to[4] = c[j].y;
+            to[0] = c[d][j].x;
+            to[4] = c[d][j].y;
         }
         float x[2][8];
-        widen_piece(p[0], x[0]);
-        widen_piece(p[1], x[1]);
-        if (s + 1 < s1) request(s + 1);
+        widen_piece(p[d][0], x[0]);
+        widen_piece(p[d][1], x[1]);
+        if (steady || s + kAhead < s1) request(d, s + kAhead, steady);
         // the wave's LDS operations execute in order: no barrier inside a wave
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -391,8 +500,8 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
             const u32x4 z = *reinterpret_cast<const u32x4 *>(table_z + g * S::rows + 8 * piece);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                minus[g][j] = stage_scaled<PLANES>(x[j], sc, z, mine + g * S::copy + (16 * j + (lane >> 2)) * S::stride + 16 * piece,
-                                                   S::plane, minus[g][j]);
+                stage_scaled<PLANES>(x[j], sc, z, mine + g * S::copy + (16 * j + (lane >> 2)) * S::stride + 16 * piece, S::plane,
+                                     minus[g][j]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -409,20 +518,46 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
                 o[0] = lds_operand(operand + pl * S::plane + 16 * m);
                 o[1] = NG == 2 ? lds_operand(operand + S::copy + pl * S::plane + 16 * m) : o[0];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) acc[r] = mfma32(o[r], decode((uint32_t)y[r][m]), acc[r]);
+                for (int r = 0; r < 2; ++r) {
+                    f32x16 &to = acc[pl ? kSums - 1 : 0][r];
+                    to = mfma32(o[r], decode((uint32_t)y[r][m]), to);
+                }
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+    };
+    // steady: all that is requested is there and whole (the last step of a matrix may not be)
+    const int partial = n_rows % S::rows ? steps1 - 1 : -1 - 2 * kAhead;
+    int s = s0;
+    while (s < s1) {
+        int end = s1 - 2 * kAhead + 1;
+        if (s + kAhead <= partial)
+            end = min(end, partial - 2 * kAhead + 1);
+        else if (s + kAhead <= partial + steps1 && both)
+            end = min(end, partial + steps1 - 2 * kAhead + 1);
+        for (; s < end; s += kAhead) {
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) step(d, s + d, std::true_type());
+        }
+#pragma unroll
+        for (int d = 0; d < kAhead; ++d)
+            if (s + d < s1) step(d, s + d, std::false_type());
+        s += kAhead;
     }
     __syncthreads();  // the staging areas become the partial results [wave][register][lane], and what is taken off
     float *red = reinterpret_cast<float *>(smem), *off = red + kBackWaves * 32 * 64;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) red[(w * 32 + i) * 64 + lane] = acc[i >> 4][i & 15];
+    for (int i = 0; i < 32; ++i) {
+        float sum = acc[0][i >> 4][i & 15];
+        if (kSums == 2) sum += acc[kSums - 1][i >> 4][i & 15];
+        red[(w * 32 + i) * 64 + lane] = sum;
+    }
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const float t = run_sum<4>(minus[g][j]);
+            float t = run_sum<4>(minus[g][j][0]);
+            if (kSums == 2) t += run_sum<4>(minus[g][j][kSums - 1]);
             if (piece == 0) off[(w * NG + g) * S::vectors + 16 * j + (lane >> 2)] = t;
         }
     __syncthreads();
@@ -448,16 +583,16 @@ struct Args {
     hipStream_t stream;
 };
 
-template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS>
+template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS, int KW>
 hipError_t launch_tile(const Args &x) {
-    using S = BackTile<VT, PLANES, NG, VB, ROWS>;
+    using S = BackTile<VT, PLANES, NG, VB, ROWS, KW>;
     static std::atomic<size_t> enabled[kMaxDevices];
-    auto kern = k_int4_back_tile<VT, OT, PLANES, NG, VB, ROWS>;
+    auto kern = k_int4_back_tile<VT, OT, PLANES, NG, VB, ROWS, KW>;
     static_assert(S::bytes <= kLdsBytes && S::codes >= NG * S::vectors * 4, "two stages, and then what is taken off");
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), S::bytes, x.device, enabled)) return e;
     const int col_tiles = (x.n_cols + 127) / 128, vec_tiles = (x.batch + S::vectors - 1) / S::vectors;
     const int per = (int)(((long long)col_tiles * vec_tiles + 7) / 8);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(per * 8)), dim3(256), S::bytes, x.stream, x.m[0], x.m[1], x.both, x.gpt,
+    hipLaunchKernelGGL(kern, dim3((unsigned)(per * 8)), dim3(S::threads), S::bytes, x.stream, x.m[0], x.m[1], x.both, x.gpt,
                        static_cast<const VT *>(x.dy), x.ntiles, x.n_rows, x.n_cols, x.ldv, x.batch, x.scale,
                        static_cast<OT *>(x.out), x.ldo, col_tiles, vec_tiles);
     return hipGetLastError();
@@ -483,14 +618,12 @@ template <typename VT, typename OT, int PLANES>
 hipError_t launch(const Args &x) {
     const long long tiles = (long long)((x.n_cols + 127) / 128) * ((x.batch + 127) / 128);
     if (x.batch <= 32 || tiles < 64) return x.gpt == 8 ? launch_split<VT, OT, PLANES, 2>(x) : launch_split<VT, OT, PLANES, 1>(x);
-    if constexpr (PLANES == 3)
-        return x.gpt == 8   ? launch_tile<VT, OT, 3, 4, 1, 32>(x)
-               : x.gpt == 4 ? launch_tile<VT, OT, 3, 2, 2, 32>(x)
-                            : launch_tile<VT, OT, 3, 1, 2, 32>(x);
-    else
-        return x.gpt == 8   ? launch_tile<VT, OT, 1, 4, 2, 32>(x)
-               : x.gpt == 4 ? launch_tile<VT, OT, 1, 2, 2, 32>(x)
-                            : launch_tile<VT, OT, 1, 1, 2, 64>(x);
+    constexpr bool one = PLANES == 1;
+    if (x.gpt == 8) return launch_tile<VT, OT, PLANES, 4, 1, 32, 1>(x);
+    if (x.gpt == 4) return one ? launch_tile<VT, OT, PLANES, 2, 1, 64, 1>(x) : launch_tile<VT, OT, PLANES, 2, 1, 32, 1>(x);
+    if constexpr (one)
+        if (tiles >= 512) return launch_tile<VT, OT, 1, 1, 2, 64, 1>(x);
+    return launch_tile<VT, OT, PLANES, 1, 1, one ? 128 : 64, 2>(x);
 }
 
 }  // namespace
@@ -522,19 +655,16 @@ hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, 
 
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,
                                int batch, float *dpre, hipStream_t stream) {
-    // (a launch holds fewer than 2^32 threads: so many vectors at a time)
-    const int64_t most = ((int64_t)1 << 31) / rows;
-    for (int64_t n = 0; n < batch; n += most) {
-        const int64_t count = (batch - n < most ? batch - n : most) * rows;
-        const dim3 grid((unsigned)((count + 255) / 256));
+    for (int n = 0; n < batch; n += 65535) {  // (as many as a grid has in that direction)
+        const dim3 grid((unsigned)((rows + 1023) / 1024), (unsigned)(batch - n < 65535 ? batch - n : 65535));
+        const float *from = pre + 2LL * n * rows;
+        float *to = dpre + 2LL * n * rows;
         if (d_dtype == RSR_BF16)
-            hipLaunchKernelGGL(k_gated_slopes<uint16_t>, grid, dim3(256), 0, stream, pre + 2 * n * rows,
-                               static_cast<const uint16_t *>(dh) + n * ldd, (long long)ldd, act, (int)rows, (long long)count,
-                               dpre + 2 * n * rows);
+            hipLaunchKernelGGL(k_gated_slopes<uint16_t>, grid, dim3(256), 0, stream, from,
+                               static_cast<const uint16_t *>(dh) + n * ldd, (long long)ldd, act, (int)rows, to);
         else
-            hipLaunchKernelGGL(k_gated_slopes<float>, grid, dim3(256), 0, stream, pre + 2 * n * rows,
-                               static_cast<const float *>(dh) + n * ldd, (long long)ldd, act, (int)rows, (long long)count,
-                               dpre + 2 * n * rows);
+            hipLaunchKernelGGL(k_gated_slopes<float>, grid, dim3(256), 0, stream, from,
+                               static_cast<const float *>(dh) + n * ldd, (long long)ldd, act, (int)rows, to);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;

@@ -174,6 +174,7 @@ void packed_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf
 // --- 4-bit weights with group scales ------------------------------------------------------
 constexpr int64_t kInt4MaxCols = (int64_t)1 << 24;
 constexpr int kInt4MaxBatch = 1 << 24;
+constexpr int64_t kInt4Behind = 64;  // bytes behind the scales that kernels read and do not use
 int64_t int4_code_bytes(int64_t rows, int64_t cols);
 int64_t int4_groups(int64_t rows, int64_t cols, int per);  // scales of a handle with groups of `per` columns
 // Null stream; flags[0] |= 1: a value out of range, flags[1] |= 1: a scale that is no bf16.
