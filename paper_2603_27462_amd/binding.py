@@ -41,6 +41,7 @@ class RsrError(RuntimeError):
 
 _lib = None
 _product = None     # rsr_call.cpp: rsr_matvec_ex with a new result on the current stream, or None if it is not built
+_int4 = _gated = None   # the same of rsr_int4_matvec and rsr_gated
 
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
@@ -127,8 +128,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
 
 
 def _load_call(lib) -> None:
-    global _product
-    _product = None
+    global _product, _int4, _gated
+    _product = _int4 = _gated = None
     try:
         loader = importlib.machinery.ExtensionFileLoader("_rsr_call", _build.CALL_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_rsr_call", loader))
@@ -143,7 +144,10 @@ def _load_call(lib) -> None:
                       % (getattr(module, "torch", "?"), _build.torch_tag()))
         return
     module.bind(ctypes.cast(lib.rsr_matvec_ex, ctypes.c_void_p).value)
-    _product = module.product
+    module.bind_int4(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.rsr_int4_matvec, lib.rsr_gated)))
+    import torch
+    _RESULTS.update({torch.float32: False, torch.bfloat16: True})
+    _product, _int4, _gated = module.product, module.int4, module.gated
 
 
 class Handle:
@@ -359,6 +363,7 @@ def rsr_matvec_ex(h: Handle, v, scale: float = 1.0, out=None, stream=None):
 
 # ---- 4-bit weights with group scales ---------------------------------------------------------
 _ACTS = {"silu": RSR_SILU, "gelu": RSR_GELU, "relu2": RSR_RELU2}
+_RESULTS = {None: False}        # types of new results, and whether they are bfloat16; filled with torch's types on loading
 
 
 def rsr_preprocess_int4(Q, scales, group: int, zeros=None) -> Handle:
@@ -440,6 +445,10 @@ def _on(device, stream, call) -> int:
 def rsr_int4_matvec(h: Handle, v, transposed: bool = False, scale: float = 1.0, dtype=None, out=None, stream=None):
     """scale * M v, or scale * M^T v: v [length] or [batch][length], float32 or bfloat16, length cols (transposed: rows).
     The result is of type `dtype`, by default float32."""
+    if out is None and stream is None and _int4 is not None and dtype in _RESULTS:
+        out = _int4(h.ptr, h.rows, h.cols, v, transposed, scale, _RESULTS[dtype])
+        if out is not None:
+            return out
     device = _int4_device(h)
     length, to = (h.rows, h.cols) if transposed else (h.cols, h.rows)
     batch, ldv, code = _vectors(v, length, device, "v")
@@ -465,13 +474,17 @@ def rsr_gated(gate: Handle, up: Handle, v, act="silu", dtype=None, out=None, pre
     """act(Mgate v) * (Mup v) for v [cols] or [batch][cols]; act: "silu", "gelu" (tanh form) or "relu2".  The result
     is of type `dtype`, by default float32.  pre: a float32 tensor [batch][2][rows] that receives both products, for
     rsr_gated_backward."""
+    act = _act_code(act)
+    if out is None and pre is None and stream is None and _gated is not None and dtype in _RESULTS:
+        out = _gated(gate.ptr, up.ptr, gate.rows, gate.cols, v, act, _RESULTS[dtype])
+        if out is not None:
+            return out
     device = _int4_device(gate, up)
     batch, ldv, code = _vectors(v, gate.cols, device, "v")
     out = _result(out, v, gate.rows, dtype)
     if pre is not None:
         _kept(pre, batch, gate.rows, device, "pre")
     ldo = gate.rows if batch <= 1 else out.stride(0)
-    act = _act_code(act)
     rc = _on(device, stream, lambda s: load_library().rsr_gated(
         gate.ptr, up.ptr, v.data_ptr(), code, act, out.data_ptr(), _dtype_code(out),
         None if pre is None else pre.data_ptr(), batch, ldv, ldo, s)) if batch else 0
