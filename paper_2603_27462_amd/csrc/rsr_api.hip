@@ -1139,8 +1139,9 @@ const char *rsr_batch_kernel_name(rsr_handle_t h, int v_dtype, int batch) {
         return nullptr;
     }
     static thread_local char name[96];
-    if (h->kind == RSR_INT4) return "k_int4_rows";
-    if (use_packed(h, v_dtype, batch, h->cols * (v_dtype == RSR_BF16 ? 2 : 4) % 16 == 0))
+    if (h->kind == RSR_INT4)
+        rsr::int4_kernel_name(h, v_dtype, batch, name, sizeof(name));
+    else if (use_packed(h, v_dtype, batch, h->cols * (v_dtype == RSR_BF16 ? 2 : 4) % 16 == 0))
         rsr::packed_kernel_name(h, v_dtype, batch, name, sizeof(name));
     else if (h->narrow)
         return v_dtype == RSR_BF16 ? "k_rsr_narrow<unsigned short>" : "k_rsr_narrow<float>";

@@ -2,6 +2,7 @@
 // matrices of one shape, h = act(Mg x) * (Mu x).
 #include "rsr_int4.h"
 
+#include <cstdio>
 #include <type_traits>
 
 namespace rsr {
@@ -671,7 +672,16 @@ struct Args {
     int out_bf16, act;
     float *pre;
     hipStream_t stream;
+    char *name;  // not null: write the name of the kernel there instead of launching it
+    size_t name_len;
 };
+
+template <typename VT, typename... Number>
+hipError_t put_name(const Args &x, const char *kernel, const char *numbers, Number... n) {
+    const int at = std::snprintf(x.name, x.name_len, "%s<%s, ", kernel, sizeof(VT) == 4 ? "float" : "unsigned short");
+    if (at > 0 && (size_t)at < x.name_len) std::snprintf(x.name + at, x.name_len - at, numbers, n...);
+    return hipSuccess;
+}
 
 // Waves that share the columns of a row group: as many as stage all of theirs at once, and more while the chip has fewer
 // than four waves per CU.
@@ -685,6 +695,7 @@ int few_wk_log2(int ntiles, int ngroups, int tiles, int most) {
 template <typename VT, int NV, int GPT, int NM>
 hipError_t launch_few(const Args &x) {
     using S = Few<VT, NV, GPT>;
+    if (x.name) return put_name<VT>(x, "k_int4_few", "%d, %d, %d>", NV, GPT, NM);
     static std::atomic<size_t> enabled[kMaxDevices];
     auto kern = k_int4_few<VT, NV, GPT, NM>;
     const int wk_log2 = few_wk_log2(x.ntiles, x.ngroups, S::tiles, few_most_waves(NM));
@@ -702,6 +713,7 @@ hipError_t launch_few(const Args &x) {
 template <typename VT, int NT, int GPT, int NM, int G>
 hipError_t launch_split_rows(const Args &x) {
     using S = Split<VT, NT, GPT>;
+    if (x.name) return put_name<VT>(x, "k_int4_split", "%d, %d, %d, %d>", NT, GPT, NM, G);
     static std::atomic<size_t> enabled[kMaxDevices];
     auto kern = k_int4_split<VT, NT, GPT, NM, G>;
     constexpr size_t staged = (size_t)kSplitWaves * S::wave_bytes, joined = (size_t)kSplitWaves * NM * G * NT * 4 * 64 * 4;
@@ -726,6 +738,7 @@ hipError_t launch_split(const Args &x) {
 template <typename VT, int GPT, int NM, bool ZEROS>
 hipError_t launch_tile_shape(const Args &x) {
     using S = Tile<VT, GPT>;
+    if (x.name) return put_name<VT>(x, "k_int4_tile", "%d, %d, %s>", GPT, NM, ZEROS ? "true" : "false");
     static std::atomic<size_t> enabled[kMaxDevices];
     auto kern = k_int4_tile<VT, GPT, NM, ZEROS>;
     constexpr size_t lds = 2 * (size_t)S::buffer;
@@ -784,6 +797,13 @@ hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float 
                        int batch, int64_t ldv, int64_t ldo, hipStream_t stream) {
     const Args x = args_of(h, nullptr, 0, v, scale, out, out_dtype, nullptr, batch, ldv, ldo, stream);
     return v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group);
+}
+
+void int4_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len) {
+    Args x = args_of(h, nullptr, 0, nullptr, 1.0f, nullptr, RSR_F32, nullptr, batch, h->cols, h->rows, nullptr);
+    x.name = buf;
+    x.name_len = len;
+    (void)(v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group));
 }
 
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,

@@ -183,6 +183,7 @@ hipError_t launch_int4_pack(const rsr_handle_s *h, const int8_t *Q, const float 
                             int64_t group, int *flags);
 hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float scale, void *out, int out_dtype,
                        int batch, int64_t ldv, int64_t ldo, hipStream_t stream);
+void int4_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len);
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,
                              void *out, int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo,
                              hipStream_t stream);
