@@ -218,10 +218,8 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
 }
 
 // ---- split: up to 64 vectors ---------------------------------------------------------------------------
-// Eight waves share the columns of G row groups (of each matrix); each stages its own columns of 16 NT vectors, half a tile at
+// WAVES waves share the columns of G row groups (of each matrix); each stages its own columns of 16 NT vectors, half a tile at
 // a time.  The vectors are the rows of the MFMA: lane l of the result holds row l % 16 of vectors 4 (l / 16) .. + 3.
-constexpr int kSplitWaves = 8;
-
 template <typename VT, int NT, int GPT>
 struct Split {
     static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
@@ -235,8 +233,8 @@ struct Split {
     static constexpr int wave_bytes = planes * plane + groups * vectors * 4;
 };
 
-template <typename VT, int NT, int GPT, int NM, int G>
-__global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
+template <typename VT, int NT, int GPT, int NM, int G, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_int4_split(
     Int4 m0, Int4 m1, const VT *__restrict__ v, int ntiles, int ngroups, int n_in, int n_out, long long ldv, int batch,
     float scale, void *__restrict__ out, int out_bf16, long long ldo, int act, float *__restrict__ pre) {
     using S = Split<VT, NT, GPT>;
@@ -246,7 +244,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int vec0 = blockIdx.y * S::vectors, group0 = blockIdx.x * G;
     const int halves = (n_in + S::cols - 1) / S::cols;
-    const int h0 = (int)((long long)halves * w / kSplitWaves), h1 = (int)((long long)halves * (w + 1) / kSplitWaves);
+    const int h0 = (int)((long long)halves * w / WAVES), h1 = (int)((long long)halves * (w + 1) / WAVES);
     const Int4 mat[2] = {m0, m1};
     unsigned char *mine = smem + w * S::wave_bytes;
     float *sums = reinterpret_cast<float *>(mine + S::planes * S::plane);  // [group][vector]
@@ -267,8 +265,8 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
             scale_row[k][g] = (rg * ntiles * kDenseRows + (lane & 15)) * GPT;
         }
     Piece<VT> p[S::loads];
-    auto request_v = [&](int h, auto steady) {
-        if (steady || (h + 1) * S::cols <= n_in) {
+    auto request_v = [&](int h, auto whole) {
+        if (whole || (h + 1) * S::cols <= n_in) {
 #pragma unroll
             for (int j = 0; j < S::loads; ++j) p[j] = load_whole_piece<VT>(row[j] + h * S::cols + 8 * piece);
         } else {
@@ -285,15 +283,11 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
                 sc[k][g] = load_scales<S::groups>(mat[k], scale_row[k][g] + (long long)(h >> 1) * kDenseRows * GPT + (h & 1) * S::groups);
             }
     };
-    constexpr int kAhead = NM * G * NT <= 2 ? 4 : NM * G * NT <= 4 ? 2 : 1;  // half tiles whose codes are on their way
+    constexpr int kAhead = NM * G * NT <= 4 ? 2 : 1;  // half tiles whose codes are on their way
     u32x4 codes[kAhead][NM][G];
     Scales<S::groups> scales[kAhead][NM][G];
     float total[NM][G][NT][4] = {};
-    if (h0 < h1) request_v(h0, std::false_type());
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d)
-        if (h0 + d < h1) request_codes(h0 + d, codes[d], scales[d]);
-    auto step = [&](int h, u32x4 (&c)[NM][G], Scales<S::groups> (&sc)[NM][G], auto steady) {
+    auto step = [&](int h, u32x4 (&c)[NM][G], Scales<S::groups> (&sc)[NM][G], auto whole) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < S::loads; ++j) {
             const int n = (j * 64 + lane) / S::pieces;
@@ -301,7 +295,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
             const float x = run_sum<kRun>(piece_sum(p[j]));
             if (piece % kRun == 0) sums[piece / kRun * S::vectors + n] = -8.0f * x;
         }
-        if (steady || h + 1 < h1) request_v(h + 1, steady);
+        request_v(min(h + 1, h1 - 1), whole);
         // the wave's LDS operations execute in order: no barrier inside a wave
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -346,18 +340,27 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (steady || h + kAhead < h1) request_codes(h + kAhead, c, sc);
+        request_codes(min(h + kAhead, h1 - 1), c, sc);
     };
-    int h = h0;
-    // (the last half tile may not be whole)
-    for (const int end = min(h1, n_in / S::cols) - 2 * kAhead + 1; h < end; h += kAhead) {
+    // Requests behind the last half tile ask for it again: a branch around them would have all loads waited for behind it.
+    auto run = [&](auto whole) __attribute__((always_inline)) {
+        request_v(h0, whole);
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d) step(h + d, codes[d], scales[d], std::true_type());
-    }
-    for (; h < h1; h += kAhead) {
+        for (int d = 0; d < kAhead; ++d) request_codes(min(h0 + d, h1 - 1), codes[d], scales[d]);
+        int h = h0;
+        for (; h + kAhead <= h1; h += kAhead) {
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d)
-            if (h + d < h1) step(h + d, codes[d], scales[d], std::false_type());
+            for (int d = 0; d < kAhead; ++d) step(h + d, codes[d], scales[d], whole);
+        }
+#pragma unroll
+        for (int d = 0; d < kAhead - 1; ++d)
+            if (h + d < h1) step(h + d, codes[d], scales[d], whole);
+    };
+    if (h0 < h1) {
+        if (h1 * S::cols <= n_in)
+            run(std::true_type());
+        else
+            run(std::false_type());
     }
     __syncthreads();  // the staging areas become the partial results [wave][matrix][group, 16 vectors, register][lane]
     float *red = reinterpret_cast<float *>(smem);
@@ -367,12 +370,12 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void k_int4_split(
         for (int i = 0; i < kAcc / NM; ++i)
             red[((w * NM + k) * (kAcc / NM) + i) * 64 + lane] = total[k][i / (4 * NT)][i / 4 % NT][i & 3];
     __syncthreads();
-    for (int i = w; i < kAcc / NM; i += kSplitWaves) {
+    for (int i = w; i < kAcc / NM; i += WAVES) {
         float sum[NM] = {};
 #pragma unroll
         for (int k = 0; k < NM; ++k)
 #pragma unroll
-            for (int u = 0; u < kSplitWaves; ++u) sum[k] += red[((u * NM + k) * (kAcc / NM) + i) * 64 + lane];
+            for (int u = 0; u < WAVES; ++u) sum[k] += red[((u * NM + k) * (kAcc / NM) + i) * 64 + lane];
         const long long r = (long long)(group0 + i / (4 * NT)) * kDenseRows + (lane & 15);
         const int n = vec0 + i / 4 % NT * 16 + 4 * (lane >> 4) + (i & 3);
         if (n >= batch || r >= n_out) continue;
@@ -506,7 +509,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void k_int4_tile(
     stage(0);
     if (stages > 1) request_v(1);
     __syncthreads();
-    auto step = [&](int s, auto steady) {
+    auto step = [&](int s, auto steady) __attribute__((always_inline)) {
         request_codes(min(s + 1, stages - 1), cn, scn);
         // the next stage goes to the other buffer, which nobody reads any more
         if constexpr (steady) {
@@ -710,18 +713,18 @@ hipError_t launch_few(const Args &x) {
     return hipGetLastError();
 }
 
-template <typename VT, int NT, int GPT, int NM, int G>
+template <typename VT, int NT, int GPT, int NM, int G, int WAVES>
 hipError_t launch_split_rows(const Args &x) {
     using S = Split<VT, NT, GPT>;
-    if (x.name) return put_name<VT>(x, "k_int4_split", "%d, %d, %d, %d>", NT, GPT, NM, G);
+    if (x.name) return put_name<VT>(x, "k_int4_split", "%d, %d, %d, %d, %d>", NT, GPT, NM, G, WAVES);
     static std::atomic<size_t> enabled[kMaxDevices];
-    auto kern = k_int4_split<VT, NT, GPT, NM, G>;
-    constexpr size_t staged = (size_t)kSplitWaves * S::wave_bytes, joined = (size_t)kSplitWaves * NM * G * NT * 4 * 64 * 4;
+    auto kern = k_int4_split<VT, NT, GPT, NM, G, WAVES>;
+    constexpr size_t staged = (size_t)WAVES * S::wave_bytes, joined = (size_t)WAVES * NM * G * NT * 4 * 64 * 4;
     constexpr size_t lds = staged > joined ? staged : joined;
     static_assert(lds <= (size_t)kLdsBytes, "staging, and then the partial results of all waves");
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
     hipLaunchKernelGGL(kern, dim3((unsigned)((x.ngroups + G - 1) / G), (unsigned)((x.batch + S::vectors - 1) / S::vectors)),
-                       dim3(kSplitWaves * 64), lds, x.stream, x.m[0], x.m[1], static_cast<const VT *>(x.v), x.ntiles, x.ngroups,
+                       dim3(WAVES * 64), lds, x.stream, x.m[0], x.m[1], static_cast<const VT *>(x.v), x.ntiles, x.ngroups,
                        x.n_in, x.n_out, x.ldv, x.batch, x.scale, x.out, x.out_bf16, x.ldo, x.act, x.pre);
     return hipGetLastError();
 }
@@ -729,10 +732,14 @@ hipError_t launch_split_rows(const Args &x) {
 template <typename VT, int GPT, int NM>
 hipError_t launch_split(const Args &x) {
     const bool few_rows = x.ngroups < 512;
-    if (x.batch <= 16 || sizeof(VT) == 4)
-        return few_rows ? launch_split_rows<VT, 1, GPT, NM, 1>(x) : launch_split_rows<VT, 1, GPT, NM, 2>(x);
-    return few_rows ? launch_split_rows<VT, sizeof(VT) == 4 ? 1 : 2, GPT, NM, 1>(x)
-                    : launch_split_rows<VT, sizeof(VT) == 4 ? 1 : 2, GPT, NM, 2>(x);
+    if (x.batch <= 16 || sizeof(VT) == 4) {
+        if constexpr (sizeof(VT) == 2)
+            if (few_rows && x.n_in >= 4096) return launch_split_rows<VT, 1, GPT, NM, 1, 16>(x);
+        return few_rows ? launch_split_rows<VT, 1, GPT, NM, 1, 8>(x) : launch_split_rows<VT, 1, GPT, NM, 2, 8>(x);
+    }
+    if constexpr (sizeof(VT) == 2)
+        return few_rows ? launch_split_rows<VT, 2, GPT, NM, 1, 8>(x) : launch_split_rows<VT, 2, GPT, NM, 2, 8>(x);
+    return hipErrorInvalidValue;
 }
 
 template <typename VT, int GPT, int NM, bool ZEROS>

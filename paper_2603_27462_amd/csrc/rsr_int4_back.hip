@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
     }
     if (stages > 2) request_scales(2);
     __syncthreads();
-    auto step = [&](int s, auto steady) {
+    auto step = [&](int s, auto steady) __attribute__((always_inline)) {
         // the next stage goes to the other buffer, which nobody reads any more
         if (steady || s + 1 < stages) {
             put_codes((s + 1) & 1);
@@ -400,12 +400,11 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
 }
 
 // ---- split: up to 32 vectors -----------------------------------------------------------------------------
-// Eight waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.
-constexpr int kBackWaves = 8;
-
-template <int PLANES, int NG>
+// WAVES waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.
+// Up to 16 vectors (VECS): the other 16 rows of the MFMA repeat them.
+template <int PLANES, int NG, int VECS>
 struct BackSplit {
-    static constexpr int rows = 32, vectors = 32;
+    static constexpr int rows = 32, vectors = VECS;
     static constexpr int stride = rows * 2 + 16;
     static constexpr int plane = vectors * stride;
     static constexpr int copy = PLANES * plane;
@@ -415,13 +414,14 @@ struct BackSplit {
     static constexpr int wave_bytes = table + NG * rows * 6;
 };
 
-template <typename VT, typename OT, int PLANES, int NG>
-__global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0, Int4 m1, int both, int gpt,
+template <typename VT, typename OT, int PLANES, int NG, int VECS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_int4_back_split(Int4 m0, Int4 m1, int both, int gpt,
                                                                        const VT *__restrict__ dy, int ntiles, int n_rows,
                                                                        int n_cols, long long ldv, int batch, float scale,
                                                                        OT *__restrict__ out, long long ldo, int col_tiles) {
-    using S = BackSplit<PLANES, NG>;
-    constexpr int kAhead = sizeof(VT) == 4 ? 2 : 4;  // steps whose loads are on their way
+    using S = BackSplit<PLANES, NG, VECS>;
+    constexpr int kPieces = VECS / 16;
+    constexpr int kAhead = PLANES == 3 && sizeof(VT) == 4 ? 1 : 2;  // steps whose loads are on their way
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -432,22 +432,22 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
     const int tile = ct >> 2, quarter = ct & 3;
     const int ngroups = (n_rows + kDenseRows - 1) / kDenseRows;
     const int steps1 = (n_rows + S::rows - 1) / S::rows, steps = both ? 2 * steps1 : steps1;
-    const int s0 = (int)((long long)steps * w / kBackWaves), s1 = (int)((long long)steps * (w + 1) / kBackWaves);
+    const int s0 = (int)((long long)steps * w / WAVES), s1 = (int)((long long)steps * (w + 1) / WAVES);
     unsigned char *mine = smem + w * S::wave_bytes;
     float *table = reinterpret_cast<float *>(mine + S::table);
     uint16_t *table_z = reinterpret_cast<uint16_t *>(table + NG * S::rows);
 
     const int piece = lane & 3;  // eight rows, of vectors lane / 4 and 16 further on
-    Piece<VT> p[kAhead][2];
+    Piece<VT> p[kAhead][kPieces];
     u32x2 c[kAhead][2];          // of two row groups
     Scales<1> sv[kAhead];        // of row lane % 32, group lane / 32
     auto pick = [&](int k) {
         return Int4{k ? m1.codes : m0.codes, k ? m1.scales : m0.scales, k ? m1.zeros : m0.zeros, k ? m1.wide : m0.wide};
     };
-    const VT *first[2];
+    const VT *first[kPieces];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) first[j] = dy + (long long)min(vec0 + 16 * j + (lane >> 2), batch - 1) * ldv;
-    auto request = [&](int slot, int s, auto steady) {
+    for (int j = 0; j < kPieces; ++j) first[j] = dy + (long long)min(vec0 + 16 * j + (lane >> 2), batch - 1) * ldv;
+    auto request = [&](int slot, int s, auto whole) {
         const int k = s >= steps1, row = (s - k * steps1) * S::rows;
         const Int4 m = pick(k);
 #pragma unroll
@@ -458,21 +458,18 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
         const long long rg = min((row + (lane & 31)) / kDenseRows, ngroups - 1);
         const long long idx = ((rg * ntiles + tile) * kDenseRows + (lane & 15)) * gpt + (NG == 2 ? 2 * quarter + half : quarter * gpt / 4);
         sv[slot] = load_scales<1>(m, idx);
-        if (steady || row + S::rows <= n_rows) {
+        if (whole || row + S::rows <= n_rows) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) p[slot][j] = load_whole_piece<VT>(first[j] + (long long)k * n_rows + row + 8 * piece);
+            for (int j = 0; j < kPieces; ++j) p[slot][j] = load_whole_piece<VT>(first[j] + (long long)k * n_rows + row + 8 * piece);
         } else {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) p[slot][j] = load_piece<VT>(first[j] + (long long)k * n_rows, row + 8 * piece, n_rows);
+            for (int j = 0; j < kPieces; ++j) p[slot][j] = load_piece<VT>(first[j] + (long long)k * n_rows, row + 8 * piece, n_rows);
         }
     };
     constexpr int kSums = PLANES == 3 ? 2 : 1;  // the top plane, and the others
     f32x16 acc[kSums][2] = {};
-    float minus[NG][2][kSums] = {};
-#pragma unroll
-    for (int d = 0; d < kAhead; ++d)
-        if (s0 + d < s1) request(d, s0 + d, std::false_type());
-    auto step = [&](int d, int s, auto steady) {
+    float minus[NG][kPieces][kSums] = {};
+    auto step = [&](int d, int s, auto whole) __attribute__((always_inline)) {
         const Int4 m = pick(s >= steps1);
         // (one group: the upper half of the lanes writes the same again)
         put_scale(table, table_z, NG == 2 ? lane : lane & 31, scale_of(sv[d], m.wide, 0), zero_of(sv[d], m, 0));
@@ -482,10 +479,10 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
             to[0] = c[d][j].x;
             to[4] = c[d][j].y;
         }
-        float x[2][8];
-        widen_piece(p[d][0], x[0]);
-        widen_piece(p[d][1], x[1]);
-        if (steady || s + kAhead < s1) request(d, s + kAhead, steady);
+        float x[kPieces][8];
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) widen_piece(p[d][j], x[j]);
+        request(d, min(s + kAhead, s1 - 1), whole);
         // the wave's LDS operations execute in order: no barrier inside a wave
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -499,13 +496,13 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
             }
             const u32x4 z = *reinterpret_cast<const u32x4 *>(table_z + g * S::rows + 8 * piece);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kPieces; ++j)
                 stage_scaled<PLANES>(x[j], sc, z, mine + g * S::copy + (16 * j + (lane >> 2)) * S::stride + 16 * piece, S::plane,
                                      minus[g][j]);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        const unsigned char *operand = mine + (lane & 31) * S::stride + 32 * half;
+        const unsigned char *operand = mine + (lane & (VECS - 1)) * S::stride + 32 * half;
         const unsigned char *code = mine + S::codes + (half * kDenseRows + (lane & 15)) * S::row_bytes + 8 * ((lane >> 4) & 1);
         i32x2 y[2];
 #pragma unroll
@@ -526,28 +523,30 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
-    // steady: all that is requested is there and whole (the last step of a matrix may not be)
-    const int partial = n_rows % S::rows ? steps1 - 1 : -1 - 2 * kAhead;
-    int s = s0;
-    while (s < s1) {
-        int end = s1 - 2 * kAhead + 1;
-        if (s + kAhead <= partial)
-            end = min(end, partial - 2 * kAhead + 1);
-        else if (s + kAhead <= partial + steps1 && both)
-            end = min(end, partial + steps1 - 2 * kAhead + 1);
-        for (; s < end; s += kAhead) {
+    // Requests behind the last step ask for it again: a branch around them would have all loads waited for behind it.
+    auto run = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
-            for (int d = 0; d < kAhead; ++d) step(d, s + d, std::true_type());
+        for (int d = 0; d < kAhead; ++d) request(d, min(s0 + d, s1 - 1), whole);
+        int s = s0;
+        for (; s + kAhead <= s1; s += kAhead) {
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) step(d, s + d, whole);
         }
 #pragma unroll
-        for (int d = 0; d < kAhead; ++d)
-            if (s + d < s1) step(d, s + d, std::false_type());
-        s += kAhead;
+        for (int d = 0; d < kAhead - 1; ++d)
+            if (s + d < s1) step(d, s + d, whole);
+    };
+    if (s0 < s1) {
+        if (n_rows % S::rows == 0)
+            run(std::true_type());
+        else
+            run(std::false_type());
     }
     __syncthreads();  // the staging areas become the partial results [wave][register][lane], and what is taken off
-    float *red = reinterpret_cast<float *>(smem), *off = red + kBackWaves * 32 * 64;
+    float *red = reinterpret_cast<float *>(smem), *off = red + WAVES * 32 * 64;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
+        if (acc_row(i & 15, 0) >= VECS || vec0 + acc_row(i & 15, 0) >= batch) continue;
         float sum = acc[0][i >> 4][i & 15];
         if (kSums == 2) sum += acc[kSums - 1][i >> 4][i & 15];
         red[(w * 32 + i) * 64 + lane] = sum;
@@ -555,17 +554,18 @@ __global__ __launch_bounds__(kBackWaves * 64, 2) void k_int4_back_split(Int4 m0,
 #pragma unroll
     for (int g = 0; g < NG; ++g)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kPieces; ++j) {
             float t = run_sum<4>(minus[g][j][0]);
             if (kSums == 2) t += run_sum<4>(minus[g][j][kSums - 1]);
             if (piece == 0) off[(w * NG + g) * S::vectors + 16 * j + (lane >> 2)] = t;
         }
     __syncthreads();
-    for (int i = w; i < 32; i += kBackWaves) {
+    for (int i = w; i < 32; i += WAVES) {
+        if (acc_row(i & 15, 0) >= VECS || vec0 + acc_row(i & 15, 0) >= batch) continue;
         const int v = acc_row(i & 15, half), r = i >> 4, col = ct * 64 + r * 32 + turned_column(lane & 31);
         float sum = 0.0f, t = 0.0f;
 #pragma unroll
-        for (int u = 0; u < kBackWaves; ++u) {
+        for (int u = 0; u < WAVES; ++u) {
             sum += red[(u * 32 + i) * 64 + lane];
             t += off[(u * NG + (NG == 2 ? r : 0)) * S::vectors + v];
         }
@@ -598,20 +598,29 @@ hipError_t launch_tile(const Args &x) {
     return hipGetLastError();
 }
 
-template <typename VT, typename OT, int PLANES, int NG>
-hipError_t launch_split(const Args &x) {
-    using S = BackSplit<PLANES, NG>;
+template <typename VT, typename OT, int PLANES, int NG, int VECS, int WAVES>
+hipError_t launch_split_waves(const Args &x) {
+    using S = BackSplit<PLANES, NG, VECS>;
     static std::atomic<size_t> enabled[kMaxDevices];
-    auto kern = k_int4_back_split<VT, OT, PLANES, NG>;
-    constexpr size_t staged = (size_t)kBackWaves * S::wave_bytes, joined = (size_t)kBackWaves * (32 * 64 + NG * S::vectors) * 4;
+    auto kern = k_int4_back_split<VT, OT, PLANES, NG, VECS, WAVES>;
+    constexpr size_t staged = (size_t)WAVES * S::wave_bytes, joined = (size_t)WAVES * (32 * 64 + NG * S::vectors) * 4;
     constexpr size_t lds = staged > joined ? staged : joined;
     static_assert(lds <= (size_t)kLdsBytes, "staging, and then the partial results of all waves");
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), lds, x.device, enabled)) return e;
     const int col_tiles = (x.n_cols + 63) / 64, per = (col_tiles + 7) / 8;
     hipLaunchKernelGGL(kern, dim3((unsigned)(per * 8), (unsigned)((x.batch + S::vectors - 1) / S::vectors)),
-                       dim3(kBackWaves * 64), lds, x.stream, x.m[0], x.m[1], x.both, x.gpt, static_cast<const VT *>(x.dy),
+                       dim3(WAVES * 64), lds, x.stream, x.m[0], x.m[1], x.both, x.gpt, static_cast<const VT *>(x.dy),
                        x.ntiles, x.n_rows, x.n_cols, x.ldv, x.batch, x.scale, static_cast<OT *>(x.out), x.ldo, col_tiles);
     return hipGetLastError();
+}
+
+template <typename VT, typename OT, int PLANES, int NG>
+hipError_t launch_split(const Args &x) {
+    if (x.batch > 16) return launch_split_waves<VT, OT, PLANES, NG, 32, 8>(x);
+    // sixteen waves where every one gets two steps, and the registers allow it
+    if constexpr (PLANES == 1 && sizeof(VT) == 2)
+        if (x.n_rows >= 1024) return launch_split_waves<VT, OT, PLANES, NG, 16, 16>(x);
+    return launch_split_waves<VT, OT, PLANES, NG, 16, 8>(x);
 }
 
 template <typename VT, typename OT, int PLANES>
