@@ -731,7 +731,9 @@ hipError_t launch_split_rows(const Args &x) {
 
 template <typename VT, int GPT, int NM>
 hipError_t launch_split(const Args &x) {
-    const bool few_rows = x.ngroups < 512;
+    // one row group per workgroup while there are fewer than two workgroups per CU
+    constexpr int kVectors = sizeof(VT) == 4 ? 16 : 32;
+    const bool few_rows = (long long)x.ngroups * ((x.batch + kVectors - 1) / kVectors) < 512;
     if (x.batch <= 16 || sizeof(VT) == 4) {
         if constexpr (sizeof(VT) == 2)
             if (few_rows && x.n_in >= 4096) return launch_split_rows<VT, 1, GPT, NM, 1, 16>(x);
@@ -760,13 +762,29 @@ hipError_t launch_tile_shape(const Args &x) {
     return hipGetLastError();
 }
 
+// Estimates in microseconds that decide between the two for more than 32 vectors.  split goes by the half tiles that
+// all workgroups together multiply; a tile's workgroup takes 1.45 us (float32 1.7) per stage of its columns, alone on its CU
+// or not, two of them 1.65 times as long.  Measured, split / tile: bf16 14336 x 4096, 64 vectors 36 / 51, 128 62 / 51;
+// 4096 x 14336, 256 vectors 143 / 157; 6912 x 2560, 256 68 / 35; 2560 x 6912, 256 48 / 79; 640 x 2560, 256 11 / 33; float32 14336 x
+// 4096, 100 vectors 116 / 111; 4096 x 14336, 100 148 / 369.
+template <bool WIDE>
+float split_us(const Args &x, int nm) {
+    const float halves = (float)((x.n_in + 127) / 128), sets = (float)(WIDE ? (x.batch + 15) / 16 : (x.batch + 31) / 32);
+    return 4.0f + (WIDE ? 0.6e-3f : 0.5e-3f) * (float)nm * (float)x.ngroups * halves * sets;
+}
+template <bool WIDE>
+float tile_us(const Args &x, int nm) {
+    const int rows = kTileWaves * 64 / nm;
+    const float groups = (float)(((long long)x.n_out + rows - 1) / rows) * (float)((x.batch + 63) / 64);
+    const float rounds = groups <= 256.0f ? 1.0f : groups <= 512.0f ? 1.65f : 1.65f * groups / 512.0f;
+    return 3.0f + (WIDE ? 1.7f * (float)((x.n_in + 63) / 64) : 1.45f * (float)((x.n_in + 127) / 128)) * rounds;
+}
+
 template <typename VT, int GPT, int NM>
 hipError_t launch_any(const Args &x) {
     if (x.batch == 1) return launch_few<VT, 1, GPT, NM>(x);
     if (x.batch <= 4) return launch_few<VT, 4, GPT, NM>(x);
-    constexpr int rows = 128 / NM;
-    const long long tiles = (long long)((x.n_out + rows - 1) / rows) * ((x.batch + 127) / 128);
-    if (x.batch <= 32 || tiles < 100) return launch_split<VT, GPT, NM>(x);
+    if (x.batch <= 32 || split_us<sizeof(VT) == 4>(x, NM) < tile_us<sizeof(VT) == 4>(x, NM)) return launch_split<VT, GPT, NM>(x);
     return x.m[0].zeros || x.m[1].zeros ? launch_tile_shape<VT, GPT, NM, true>(x) : launch_tile_shape<VT, GPT, NM, false>(x);
 }
 

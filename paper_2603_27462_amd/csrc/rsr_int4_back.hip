@@ -623,16 +623,40 @@ hipError_t launch_split(const Args &x) {
     return launch_split_waves<VT, OT, PLANES, NG, 16, 8>(x);
 }
 
+// Estimates in microseconds.  A wave of split takes 0.85 us (three planes 1.4) per 32 rows, a workgroup of a tile about as
+// long per stage whatever its shape, and rounds of more workgroups than the chip runs at once follow one another.  Measured for groups of
+// 128 columns, split / tiles of 64 vectors / of 128: bf16 14336 x 4096, 64 vectors 46 / 124 / 343, 256 vectors 89 / 122 / 290; 4096 x
+// 14336, 64 vectors 32 / 41 / 106, 256 104 / 60 / 90, 2048 - / 399 / 317; 6912 x 2560, 256 46 / 64 / 145; 2560 x 6912, 256 43 / 29 /
+// 60; 640 x 2560, 128 6.7 / 11 / 19; float32 4096 x 14336, 40 vectors 48 / 98, 100 vectors 94 / 92.
+float rounds_of(int columns, int vectors, const Args &x, int at_once) {
+    const float groups = (float)((x.n_cols + columns - 1) / columns) * (float)((x.batch + vectors - 1) / vectors);
+    return groups <= (float)at_once ? 1.0f : groups / (float)at_once;
+}
+float tile_us(const Args &x, int rows, int vectors, float stage_us, int at_once) {
+    return 3.0f + stage_us * (float)((x.n_rows + rows - 1) / rows) * (x.both ? 2.0f : 1.0f) * rounds_of(128, vectors, x, at_once);
+}
+
 template <typename VT, typename OT, int PLANES>
 hipError_t launch(const Args &x) {
-    const long long tiles = (long long)((x.n_cols + 127) / 128) * ((x.batch + 127) / 128);
-    if (x.batch <= 32 || tiles < 64) return x.gpt == 8 ? launch_split<VT, OT, PLANES, 2>(x) : launch_split<VT, OT, PLANES, 1>(x);
     constexpr bool one = PLANES == 1;
-    if (x.gpt == 8) return launch_tile<VT, OT, PLANES, 4, 1, 32, 1>(x);
-    if (x.gpt == 4) return one ? launch_tile<VT, OT, PLANES, 2, 1, 64, 1>(x) : launch_tile<VT, OT, PLANES, 2, 1, 32, 1>(x);
+    const float split = 4.0f + (one ? 0.85f : 1.4f) * (float)x.n_rows / 256.0f * (x.both ? 2.0f : 1.0f) * rounds_of(64, 32, x, 256);
+    const bool few = x.batch <= 32;
+    if (x.gpt == 8) {
+        if (few || split < tile_us(x, 32, 64, 1.0f, 512)) return launch_split<VT, OT, PLANES, 2>(x);
+        return launch_tile<VT, OT, PLANES, 4, 1, 32, 1>(x);
+    }
+    if (x.gpt == 4) {
+        constexpr int rows = one ? 64 : 32;
+        if (few || split < tile_us(x, rows, 64, 1.2f, 512)) return launch_split<VT, OT, PLANES, 1>(x);
+        return launch_tile<VT, OT, PLANES, 2, 1, rows, 1>(x);
+    }
+    constexpr int rows = one ? 128 : 64;
+    const float small = tile_us(x, rows, 64, one ? 1.1f : 1.4f, 256);
+    const float large = one ? tile_us(x, 64, 128, 1.35f, 512) : small;
+    if (few || split < (small < large ? small : large)) return launch_split<VT, OT, PLANES, 1>(x);
     if constexpr (one)
-        if (tiles >= 512) return launch_tile<VT, OT, 1, 1, 2, 64, 1>(x);
-    return launch_tile<VT, OT, PLANES, 1, 1, one ? 128 : 64, 2>(x);
+        if (large < small) return launch_tile<VT, OT, 1, 1, 2, 64, 1>(x);
+    return launch_tile<VT, OT, PLANES, 1, 1, rows, 2>(x);
 }
 
 }  // namespace
