@@ -10,6 +10,8 @@ namespace rsr {
 namespace {
 
 // ---- packing --------------------------------------------------------------------------------------
+typedef uint32_t u32x2_bytes __attribute__((ext_vector_type(2), aligned(1)));
+
 // One thread per (row group, tile, lane): its eight dwords.
 __global__ __launch_bounds__(256) void k_int4_pack(const int8_t *__restrict__ Q, int64_t rows, int64_t cols,
                                                    int64_t ntiles, int64_t threads, uint32_t *__restrict__ codes,
@@ -19,21 +21,31 @@ __global__ __launch_bounds__(256) void k_int4_pack(const int8_t *__restrict__ Q,
     const int lane = (int)(gid & 63);
     const int64_t gt = gid >> 6, G = gt / ntiles, t = gt - G * ntiles;
     const int64_t i = G * kDenseRows + (lane & 15);
-    bool bad = false;
+    uint32_t bad = 0, word[kInt4Steps];
 #pragma unroll
     for (int d = 0; d < kInt4Steps; ++d) {
         const int64_t j0 = t * kInt4Tile + 32 * d + 8 * (lane >> 4);
-        uint32_t word = 0x88888888u;  // zero
+        uint32_t x[2] = {0, 0};
         if (i < rows) {
-            for (int e = 0; e < 8 && j0 + e < cols; ++e) {
-                const int q = Q[i * cols + j0 + e];
-                bad |= q < -8 || q > 7;
-                const int at = 8 * (e & 3) + 4 * (e >> 2);
-                word = (word & ~(15u << at)) | ((uint32_t)(q + 8) & 15u) << at;
+            const int8_t *from = Q + i * cols + j0;
+            if (j0 + 8 <= cols) {
+                const u32x2_bytes y = *reinterpret_cast<const u32x2_bytes *>(from);
+                x[0] = y.x;
+                x[1] = y.y;
+            } else {
+                for (int e = 0; e < 8 && j0 + e < cols; ++e) x[e >> 2] |= (uint32_t)(uint8_t)from[e] << (8 * (e & 3));
             }
         }
-        codes[gt * kInt4TileDwords + (d >> 2) * 256 + lane * 4 + (d & 3)] = word;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            x[h] = ((x[h] & 0x7f7f7f7fu) + 0x08080808u) ^ (x[h] & 0x80808080u);  // 8 more, byte by byte
+            bad |= x[h] & 0xf0f0f0f0u;
+        }
+        word[d] = (x[0] & 0x0f0f0f0fu) | (x[1] & 0x0f0f0f0fu) << 4;
     }
+    u32x4 *to = reinterpret_cast<u32x4 *>(codes + gt * kInt4TileDwords) + lane;
+    to[0] = u32x4{word[0], word[1], word[2], word[3]};
+    to[64] = u32x4{word[4], word[5], word[6], word[7]};
     if (bad) atomicOr(flags, 1);
 }
 
