@@ -243,7 +243,7 @@ int rsr_preprocess_into(rsr_handle_t h, const int8_t *M);
  *   zeros   DEVICE int8, as scales, entries -8..7; or NULL: all zero
  *   group   columns that share a scale: a positive multiple of 32, or any number >= cols (one scale per row); the last group
  *           of a row may be shorter
- *   rows <= 2^30, cols <= 2^24 (RSR_EUNSUPPORTED beyond)
+ *   rows <= 2^24, cols <= 2^24 (RSR_EUNSUPPORTED beyond)
  *
  * All three are borrowed until the call returns.  Runs on the null stream and synchronises.  An entry, zero point or scale out
  * of range: RSR_EVALUE.
@@ -310,7 +310,7 @@ int rsr_gated(rsr_handle_t gate, rsr_handle_t up, const void *v, int v_dtype, in
  *          need; may be `pre` itself, else they may not overlap
  *   dv     DEVICE, dv_dtype, [batch] vectors of length cols, lddv apart; or NULL: only dpre is computed
  * With a float32 dv nothing is rounded below float32; for a bf16 one da and db, scaled, are rounded to bf16 once, as above.
- * Two launches on `stream`; the rest as for rsr_int4_matvec.
+ * Two launches on `stream` (more for batches beyond what a launch holds, as everywhere here); the rest as for rsr_int4_matvec.
  */
 int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, const void *dout, int d_dtype, int act,
                        float *dpre, void *dv, int dv_dtype, int batch, int64_t ldd, int64_t lddv, void *stream);

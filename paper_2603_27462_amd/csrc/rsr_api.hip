@@ -915,7 +915,7 @@ int rsr_matvec_ex(rsr_handle_t h, const void *v, int v_dtype, float scale, void 
 rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int8_t *zeros, int64_t rows, int64_t cols,
                                  int64_t group) {
     if (!Q || !scales || rows < 1 || cols < 1 || group < 1) { fail(RSR_EINVAL); return nullptr; }
-    if (rows > (int64_t)1 << 30 || cols > rsr::kInt4MaxCols || (group < cols && group % 32)) {
+    if (rows > rsr::kInt4MaxRows || cols > rsr::kInt4MaxCols || (group < cols && group % 32)) {
         fail(RSR_EUNSUPPORTED);
         return nullptr;
     }

@@ -801,8 +801,25 @@ hipError_t launch_any(const Args &x) {
 }
 
 template <typename VT, int NM>
-hipError_t launch_groups(const Args &x, int group) {
+hipError_t launch_all(const Args &x, int group) {
     return group == 32 ? launch_any<VT, 8, NM>(x) : group == 64 ? launch_any<VT, 4, NM>(x) : launch_any<VT, 2, NM>(x);
+}
+
+// (A launch holds fewer than 2^32 threads, at most 512 per row group and 16 vectors, and 65535 sets of vectors: so many at a time.)
+template <typename VT, int NM>
+hipError_t launch_groups(const Args &x, int group) {
+    const long long sets = (1LL << 31) / (512LL * x.ngroups);
+    const int most = 16 * (int)(sets < 4 ? 4 : sets > 32768 ? 32768 : sets);
+    if (x.batch <= most) return launch_all<VT, NM>(x, group);
+    Args y = x;
+    for (int n = 0; n < x.batch; n += most) {
+        y.batch = x.batch - n < most ? x.batch - n : most;
+        y.v = static_cast<const VT *>(x.v) + n * x.ldv;
+        y.out = static_cast<unsigned char *>(x.out) + n * x.ldo * (x.out_bf16 ? 2 : 4);
+        if (x.pre) y.pre = x.pre + 2LL * n * x.n_out;
+        if (hipError_t e = launch_all<VT, NM>(y, group)) return e;
+    }
+    return hipSuccess;
 }
 
 Args args_of(const rsr_handle_s *a, const rsr_handle_s *b, int act, const void *v, float scale, void *out, int out_dtype,

@@ -637,7 +637,7 @@ float tile_us(const Args &x, int rows, int vectors, float stage_us, int at_once)
 }
 
 template <typename VT, typename OT, int PLANES>
-hipError_t launch(const Args &x) {
+hipError_t launch_all(const Args &x) {
     constexpr bool one = PLANES == 1;
     const float split = 4.0f + (one ? 0.85f : 1.4f) * (float)x.n_rows / 256.0f * (x.both ? 2.0f : 1.0f) * rounds_of(64, 32, x, 256);
     const bool few = x.batch <= 32;
@@ -657,6 +657,23 @@ hipError_t launch(const Args &x) {
     if constexpr (one)
         if (large < small) return launch_tile<VT, OT, 1, 1, 2, 64, 1>(x);
     return launch_tile<VT, OT, PLANES, 1, 1, rows, 2>(x);
+}
+
+// (A launch holds fewer than 2^32 threads, at most 1024 per 64 columns and 32 vectors, and 65535 sets of vectors: so many at
+// a time.)
+template <typename VT, typename OT, int PLANES>
+hipError_t launch(const Args &x) {
+    const long long sets = (1LL << 31) / (1024LL * ((x.n_cols + 63) / 64));
+    const int most = 32 * (int)(sets > 16384 ? 16384 : sets);
+    if (x.batch <= most) return launch_all<VT, OT, PLANES>(x);
+    Args y = x;
+    for (int n = 0; n < x.batch; n += most) {
+        y.batch = x.batch - n < most ? x.batch - n : most;
+        y.dy = static_cast<const VT *>(x.dy) + n * x.ldv;
+        y.out = static_cast<OT *>(x.out) + n * x.ldo;
+        if (hipError_t e = launch_all<VT, OT, PLANES>(y)) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -688,8 +705,11 @@ hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, 
 
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,
                                int batch, float *dpre, hipStream_t stream) {
-    for (int n = 0; n < batch; n += 65535) {  // (as many as a grid has in that direction)
-        const dim3 grid((unsigned)((rows + 1023) / 1024), (unsigned)(batch - n < 65535 ? batch - n : 65535));
+    // (a launch holds fewer than 2^32 threads, and 65535 vectors: so many at a time)
+    const int64_t blocks = (rows + 1023) / 1024, fit = ((int64_t)1 << 31) / (256 * blocks);
+    const int most = (int)(fit < 65535 ? fit : 65535);
+    for (int n = 0; n < batch; n += most) {
+        const dim3 grid((unsigned)blocks, (unsigned)(batch - n < most ? batch - n : most));
         const float *from = pre + 2LL * n * rows;
         float *to = dpre + 2LL * n * rows;
         if (d_dtype == RSR_BF16)

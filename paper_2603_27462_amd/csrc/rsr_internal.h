@@ -172,7 +172,7 @@ void packed_launch_shape(const rsr_handle_s *h, int v_dtype, int *workgroups, in
 void packed_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len);
 
 // --- 4-bit weights with group scales ------------------------------------------------------
-constexpr int64_t kInt4MaxCols = (int64_t)1 << 24;
+constexpr int64_t kInt4MaxRows = (int64_t)1 << 24, kInt4MaxCols = (int64_t)1 << 24;
 constexpr int kInt4MaxBatch = 1 << 24;
 constexpr int64_t kInt4Behind = 64;  // bytes behind the scales that kernels read and do not use
 int64_t int4_code_bytes(int64_t rows, int64_t cols);

@@ -542,3 +542,36 @@ def test_codes_beyond_32_bits():
     y = torch.zeros(rows, device=DEV)
     y[5] = y[rows // 2] = y[-3] = 1.0
     assert torch.equal(rsr.rsr_int4_matvec(h, y, transposed=True), (Q[5].float() + Q[rows // 2] + Q[-3]))
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 24) - 5, 33), (70, (1 << 24) - 300)])
+def test_the_largest_sizes(rows, cols):
+    """Row and column counts at the limits, with vectors for every kernel: several launches where one does not hold them."""
+    g = _gen(50)
+    Q = torch.randint(-8, 8, (rows, cols), generator=g, device=DEV, dtype=torch.int8)
+    s = torch.ones((rows, 1), device=DEV)
+    h = rsr.rsr_preprocess_int4(Q, s, cols)
+    tall = rows > cols
+    for batch in (1, 4, 20, 90):
+        # one element in each vector: products are columns, or rows, of Q
+        at = torch.randint(0, cols if tall else rows, (batch,), generator=g, device=DEV)
+        x = torch.zeros((batch, cols if tall else rows), device=DEV, dtype=BF16)
+        x[torch.arange(batch, device=DEV), at] = 1.0
+        got = rsr.rsr_int4_matvec(h, x, transposed=not tall, dtype=BF16)
+        for n in range(batch):
+            assert torch.equal(got[n], (Q[:, at[n]] if tall else Q[at[n]]).to(BF16))
+
+
+def test_many_vectors():
+    """More vectors than a grid has in one direction, and than one launch of the activation's gradient."""
+    wg, wu, gate, up = _pair(rows=40, cols=33, group=32)
+    batch = 66000
+    x, dh = _vectors(batch, 33, BF16, 1, 0, True), _vectors(batch, 40, BF16, 2, 0, True)
+    assert torch.equal(rsr.rsr_int4_matvec(gate, x, dtype=BF16), (x.double() @ _matrix(wg, 32)[0].t()).to(BF16))
+    assert torch.equal(rsr.rsr_int4_matvec(gate, dh, transposed=True, dtype=BF16), (dh.double() @ _matrix(wg, 32)[0]).to(BF16))
+    pre = torch.empty((batch, 2, 40), device=DEV)
+    h = rsr.rsr_gated(gate, up, x, "relu2", pre=pre)
+    assert torch.equal(h[-100:], rsr.rsr_gated(gate, up, x[-100:], "relu2"))
+    dv, dpre = rsr.rsr_gated_backward(gate, up, pre, dh, "relu2")
+    assert torch.equal(dpre[-3:, 1], dh[-3:].float() * torch.relu(pre[-3:, 0]) ** 2)
+    assert torch.equal(dpre[:3, 1], dh[:3].float() * torch.relu(pre[:3, 0]) ** 2)

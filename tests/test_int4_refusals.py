@@ -22,7 +22,7 @@ def test_preprocess_invalid(args):
     assert _preprocess(**args) == EINVAL
 
 
-@pytest.mark.parametrize("args", [dict(group=31), dict(group=48), dict(rows=(1 << 30) + 1), dict(cols=(1 << 24) + 1),
+@pytest.mark.parametrize("args", [dict(group=31), dict(group=48), dict(rows=(1 << 24) + 1), dict(rows=(1 << 30) + 1), dict(cols=(1 << 24) + 1),
                                   dict(cols=1 << 40)])
 def test_preprocess_beyond_the_limits(args):
     assert _preprocess(**args) == EUNSUPPORTED
