@@ -85,6 +85,10 @@ __global__ __launch_bounds__(256) void k_int4_pack_scales(const float *__restric
 }
 
 // ---- few: up to four vectors ------------------------------------------------------------------------
+// Bound by memory and the start-up of a launch: 4096 x 14336, one bf16 vector 8.4 us with the codes from HBM (3.6 TB/s; a plain
+// read of them in one launch 6.2), gate and up of 6912 x 2560 6.7 us (4.6); 367 vector instructions and 28 MFMAs per wave.
+// Requests beyond a wave's tiles instead of branches around them, as in the other kernels, lose here, where a wave has one
+// to four tiles: 640 x 2560 3.5 -> 4.9 us.
 // A wave takes 16 rows (of both matrices, if there are two) and a share of the columns; `wk` waves of a workgroup share
 // the columns of a row group and add their partial results at the end, the only place where waves wait for each other.
 // Every wave stages its own columns of v, and the sums of v over the groups, in LDS of its own.  The vectors are the rows of
@@ -232,6 +236,8 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
 // ---- split: up to 64 vectors ---------------------------------------------------------------------------
 // WAVES waves share the columns of G row groups (of each matrix); each stages its own columns of 16 NT vectors, half a tile at
 // a time.  The vectors are the rows of the MFMA: lane l of the result holds row l % 16 of vectors 4 (l / 16) .. + 3.
+// 14336 x 4096, 16 bf16 vectors, groups of 64: 14.8 us (a plain read of the codes 6.5); a step's staging, decoding and scaling are
+// about 160 vector instructions per two row groups, and there are few steps to a wave.
 template <typename VT, int NT, int GPT>
 struct Split {
     static constexpr int planes = sizeof(VT) == 4 ? 3 : 1;
@@ -413,6 +419,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_int4_split(
 // buffered, one barrier per stage, and their sums over the groups with them; the codes come straight from memory, every
 // wave those of its own rows.  A stage's group is decoded once into registers for all of the wave's vectors; its sum starts at
 // minus eight times the vector's, and is scaled and added to the result's.
+// 4096 x 14336, 2048 bf16 vectors, groups of 128: 270 us (890 TFLOP/s, a library product 191); 284 vector instructions to 32 MFMAs
+// per wave and stage, MFMA busy 44 %, vector issue 48 %, hardly at the same time.  Measured against it: 256 rows x 128 vectors in
+// eight waves 299, 128 x 128 in four with stages of 64 columns 429, 32 rows x 128 vectors per wave 302, 64 x 128 per wave with all 512
+// registers 358; the next stage written between or behind the products 277 to 303; sums scaled behind the branches of a stage
+// (where the compiler moves them if it may) spill 700 bytes.  Groups of 32: 392 us, a sum of 32 columns is two MFMAs and 16
+// multiplications.
 constexpr int kTileWaves = 4, kTileVecs = 2;  // 64 rows each; blocks of 32 vectors
 
 template <typename VT, int GPT>

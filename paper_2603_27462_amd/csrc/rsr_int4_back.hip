@@ -8,7 +8,8 @@ namespace rsr {
 
 namespace {
 
-// (da, db) from (a, b) and dh, four elements of a vector per thread; dpre may be pre.
+// (da, db) from (a, b) and dh, four elements of a vector per thread; dpre may be pre.  6912 x 1024, bf16 dh: 127 MB in 20 us, a large
+// copy's rate.
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
@@ -153,6 +154,12 @@ __device__ __forceinline__ void put_scale(float *scales, uint16_t *zeros, int at
 // first eight rows of every row group and one the others, and they add up at the end.  A stage is ROWS rows of one matrix: dy
 // scaled for each of the NG groups of the 128 columns, and the codes.  One barrier per stage.
 // Three planes: the top one has sums of its own, whose products have few bits and add up almost exactly.
+// Scaling and rounding dy costs 25 vector instructions per eight elements and group of columns, whatever the tile, that is about
+// as long as the products of a group of 128; a tile of groups of 64 or 32 does it two or four times.  4096 x 14336, 2048 bf16
+// vectors, groups of 128: 317 us (759 TFLOP/s, a library product 191 to 216 us; per wave and stage of 64 rows 230 vector
+// instructions to 16 MFMAs, MFMA busy 35 %), of 64 437 us, of 32 789.  Not kept: the operands of a stage read before the
+// next one is written (334 us, and 355 instead of 302 for a training step of 6912 x 2560: its loads are asked for later), two stages of
+// loads on their way (336 and 343: more registers, fewer waves), three waves per SIMD enforced (no difference).
 template <typename VT, int PLANES, int NG, int VB, int ROWS, int KW>
 struct BackTile {
     static constexpr int threads = 256 * KW;
@@ -400,7 +407,9 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
 }
 
 // ---- split: up to 32 vectors -----------------------------------------------------------------------------
-// WAVES waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.
+// WAVES waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.  Bound by the chain
+// of a step (scales, dy, operands: three turns through LDS) and what is around it: 4096 x 14336, one bf16 vector 13.7 us (2.2 TB/s,
+// a plain read of the codes 6.2), where branches around its requests had all loads waited for 22.5.
 // Up to 16 vectors (VECS): the other 16 rows of the MFMA repeat them.
 template <int PLANES, int NG, int VECS>
 struct BackSplit {
@@ -623,11 +632,12 @@ hipError_t launch_split(const Args &x) {
     return launch_split_waves<VT, OT, PLANES, NG, 16, 8>(x);
 }
 
-// Estimates in microseconds.  A wave of split takes 0.85 us (three planes 1.4) per 32 rows, a workgroup of a tile about as
+// Estimates in microseconds.  A wave of split takes 0.92 us (three planes 1.4) per 32 rows, a workgroup of a tile about as
 // long per stage whatever its shape, and rounds of more workgroups than the chip runs at once follow one another.  Measured for groups of
 // 128 columns, split / tiles of 64 vectors / of 128: bf16 14336 x 4096, 64 vectors 46 / 124 / 343, 256 vectors 89 / 122 / 290; 4096 x
-// 14336, 64 vectors 32 / 41 / 106, 256 104 / 60 / 90, 2048 - / 399 / 317; 6912 x 2560, 256 46 / 64 / 145; 2560 x 6912, 256 43 / 29 /
-// 60; 640 x 2560, 128 6.7 / 11 / 19; float32 4096 x 14336, 40 vectors 48 / 98, 100 vectors 94 / 92.
+// 14336, 64 vectors 32 / 41 / 106, 256 104 / 60 / 90, 2048 - / 399 / 317; 6912 x 2560, 256 46 / 64 / 145, 512 68 / 63, 2048 - / 140 / 157; 2560 x 6912, 256 43 / 29 /
+// 60; 640 x 2560, 128 6.7 / 11 / 19; float32 4096 x 14336, 40 vectors 48 / 98, 100 vectors 94 / 92.  Two workgroups of eight waves do
+// not fit a CU together, but the CUs that finish early take up to a quarter of a round more at little cost, hence 320 for 256 CUs.
 float rounds_of(int columns, int vectors, const Args &x, int at_once) {
     const float groups = (float)((x.n_cols + columns - 1) / columns) * (float)((x.batch + vectors - 1) / vectors);
     return groups <= (float)at_once ? 1.0f : groups / (float)at_once;
@@ -639,7 +649,7 @@ float tile_us(const Args &x, int rows, int vectors, float stage_us, int at_once)
 template <typename VT, typename OT, int PLANES>
 hipError_t launch_all(const Args &x) {
     constexpr bool one = PLANES == 1;
-    const float split = 4.0f + (one ? 0.85f : 1.4f) * (float)x.n_rows / 256.0f * (x.both ? 2.0f : 1.0f) * rounds_of(64, 32, x, 256);
+    const float split = 4.0f + (one ? 0.92f : 1.4f) * (float)x.n_rows / 256.0f * (x.both ? 2.0f : 1.0f) * rounds_of(64, 32, x, 256);
     const bool few = x.batch <= 32;
     if (x.gpt == 8) {
         if (few || split < tile_us(x, 32, 64, 1.0f, 512)) return launch_split<VT, OT, PLANES, 2>(x);
@@ -651,7 +661,7 @@ hipError_t launch_all(const Args &x) {
         return launch_tile<VT, OT, PLANES, 2, 1, rows, 1>(x);
     }
     constexpr int rows = one ? 128 : 64;
-    const float small = tile_us(x, rows, 64, one ? 1.1f : 1.4f, 256);
+    const float small = tile_us(x, rows, 64, one ? 1.1f : 1.4f, one ? 320 : 256);
     const float large = one ? tile_us(x, 64, 128, 1.35f, 512) : small;
     if (few || split < (small < large ? small : large)) return launch_split<VT, OT, PLANES, 1>(x);
     if constexpr (one)
