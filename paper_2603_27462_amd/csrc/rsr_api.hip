@@ -919,6 +919,7 @@ rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int
         fail(RSR_EUNSUPPORTED);
         return nullptr;
     }
+    if (group > cols) group = cols;  // one scale per row; sums below stay in 64 bits
     rsr_handle_s *h = new (std::nothrow) rsr_handle_s();
     if (!h) { fail(RSR_ENOMEM); return nullptr; }
     h->magic = rsr::kMagic;

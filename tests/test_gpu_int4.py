@@ -575,3 +575,13 @@ def test_many_vectors():
     dv, dpre = rsr.rsr_gated_backward(gate, up, pre, dh, "relu2")
     assert torch.equal(dpre[-3:, 1], dh[-3:].float() * torch.relu(pre[-3:, 0]) ** 2)
     assert torch.equal(dpre[:3, 1], dh[:3].float() * torch.relu(pre[:3, 0]) ** 2)
+
+
+@pytest.mark.parametrize("group", [300, 1 << 31, (1 << 63) - 1])
+def test_one_scale_per_row(group):
+    w = _weight(70, 300, 300, True, 90)
+    h = _handle(w, 300) if group == 300 else rsr.rsr_preprocess_int4(w[0], w[1], group, zeros=w[2])
+    M, sizes = _matrix(w, 300)
+    v = torch.randint(-3, 4, (3, 300), generator=_gen(91), device=DEV).float()
+    got = rsr.rsr_int4_matvec(h, v).double()
+    assert bool(((got - v.double() @ M.t()).abs() <= 300 * 2.0 ** -24 * (v.double().abs() @ sizes.t())).all())
