@@ -43,14 +43,15 @@ class RsrLinear(torch.nn.Module):
 
 
 def _rows(x: torch.Tensor, length: int) -> torch.Tensor:
-    """x as [tokens][length] with unit inner stride"""
+    """x as [tokens][length] with unit inner stride, one token behind the other (an expanded x has them all in one place)"""
     if x.shape[-1] != length:
         raise ValueError("last dimension of x must be %d" % length)
     tokens = 1
     for n in x.shape[:-1]:
         tokens *= n
     flat = x.reshape(tokens, length)
-    return flat if length == 1 or flat.stride(-1) == 1 else flat.contiguous()
+    whole = (length == 1 or flat.stride(-1) == 1) and (tokens <= 1 or flat.stride(0) >= length)
+    return flat if whole else flat.contiguous()
 
 
 class _Int4Product(torch.autograd.Function):

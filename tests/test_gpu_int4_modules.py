@@ -199,3 +199,26 @@ def test_blocks_that_do_not_fit():
         RsrGatedMlp(gate, up, down)(torch.zeros((2, 319), device=DEV))
     with pytest.raises(TypeError):
         down(torch.zeros((2, 700), device=DEV, dtype=torch.float16))
+
+
+def test_tokens_in_one_place():
+    """one token, expanded to several, and a gradient that is the same for all tokens"""
+    layer, M = _layer(64, 96, 32, 30)
+    token = torch.randn(96, generator=_gen(31), device=DEV, requires_grad=True)
+    w = torch.randn(64, generator=_gen(32), device=DEV)
+    y = layer(token.expand(5, 96))
+    want = layer(token.detach().expand(5, 96).contiguous())
+    assert torch.equal(y, want)
+    (y.sum(dim=0) * w).sum().backward()
+    size = w.double().abs() @ M.abs().clamp(min=24 * 1.5 / (5 * 96 ** 0.5))
+    # five gradients of sums of 64 products, rounded, and their sum
+    assert bool(((token.grad.double() - 5 * (w.double() @ M)).abs() <= 5 * (96 + 6) * 2.0 ** -24 * size).all())
+    block = RsrGatedMlp(*_block()[:3])
+    x = torch.randn(3, 320, generator=_gen(33), device=DEV, requires_grad=True)
+    block(x).sum(dim=0).pow(2).sum().backward()
+    got, x.grad = x.grad, None
+    y = block(x)
+    y.backward((2 * y.detach().sum(dim=0)).expand(3, -1).contiguous())
+    assert torch.equal(got, x.grad)
+    overlapping = torch.randn(200, generator=_gen(34), device=DEV).as_strided((4, 96), (32, 1))
+    assert torch.equal(layer(overlapping), layer(overlapping.clone()))
