@@ -711,7 +711,9 @@ hipError_t put_name(const Args &x, const char *kernel, const char *numbers, Numb
 }
 
 // Waves that share the columns of a row group: as many as stage all of theirs at once, and more while the chip has fewer
-// than four waves per CU.
+// than four waves per CU.  Measured, one bf16 vector, 1 / 2 / 4 / 8 / 16 waves: 4096 x 14336 30.5 / 17.5 / 12.0 / 9.2 / 8.4 us, 14336 x 4096
+// 12.0 / 9.1 / 8.4 / 9.1 / 12.4 (4 are taken), 2560 x 6912 16.4 / 10.1 / 6.4 / 5.2 / 5.1, 640 x 2560 7.2 / 4.9 / 3.4 / 3.4 / 3.6; four vectors on
+// 4096 x 14336 41 / 23 / 13 / 11 / 10.
 int few_wk_log2(int ntiles, int ngroups, int tiles, int most) {
     int log2 = 0;
     while (2 << log2 <= most && (ntiles + tiles - 1) / tiles > 1 << log2) ++log2;
@@ -755,7 +757,10 @@ hipError_t launch_split_rows(const Args &x) {
 
 template <typename VT, int GPT, int NM>
 hipError_t launch_split(const Args &x) {
-    // one row group per workgroup while there are fewer than two workgroups per CU
+    // one row group per workgroup while there are fewer than two workgroups per CU, and sixteen waves for it where each gets two
+    // steps.  Measured, two row groups / one / one with sixteen waves: 4096 x 14336, 8 vectors 15.7 / 13.4 / 11.6 us, 16 vectors 16.5 /
+    // 14.0 / 13.6, 32 23.6 / 20.1 / -, 64 23.8 / 37.0 / -; 14336 x 4096, 16 vectors 13.8 / 16.0 / 20.0, 32 19.7 / 26.1 / -; 2560 x 6912, 16
+    // 9.5 / 8.0 / 8.1; 640 x 2560, 16 5.5 / 4.7 / 5.1.
     constexpr int kVectors = sizeof(VT) == 4 ? 16 : 32;
     const bool few_rows = (long long)x.ngroups * ((x.batch + kVectors - 1) / kVectors) < 512;
     if (x.batch <= 16 || sizeof(VT) == 4) {
