@@ -271,8 +271,8 @@ rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int
  *
  * Sums are float32 and the weights are exact: codes minus zero points are multiplied as whole numbers and sums over
  * a group are scaled.  The transpose sums over the rows, whose scales differ, so there it is the vector that is scaled:
- * in float32, but rounded to bf16 (half a step, 2^-8) where v and out are both bf16; with float32 on either side nothing is
- * rounded below float32.  Every entry is multiplied, zeros too: an infinite or NaN element of a vector
+ * in float32, and where v and out are both bf16 it is kept to 16 bits, which hold the product with a bf16 scale exactly
+ * and any other to 2^-16; with float32 on either side nothing is rounded below float32.  Every entry is multiplied, zeros too: an infinite or NaN element of a vector
  * leaves none of its results finite (others of the batch are never touched), and elements beyond 2^120 may.  A float32 element below
  * 2^-109 loses its bits below 2^-133.  The order of the sums depends on the number of vectors, as for rsr_matvec_ex; the
  * same call gives the same bits every time.
@@ -309,7 +309,7 @@ int rsr_gated(rsr_handle_t gate, rsr_handle_t up, const void *v, int v_dtype, in
  *   dpre   DEVICE float32 [batch][2][rows], overwritten: da and db, which adapters beside the projections
  *          need; may be `pre` itself, else they may not overlap
  *   dv     DEVICE, dv_dtype, [batch] vectors of length cols, lddv apart; or NULL: only dpre is computed
- * With a float32 dv nothing is rounded below float32; for a bf16 one da and db, scaled, are rounded to bf16 once, as above.
+ * With a float32 dv nothing is rounded below float32; for a bf16 one da and db, scaled, are kept to 16 bits (2^-16).
  * Two launches on `stream` (more for batches beyond what a launch holds, as everywhere here); the rest as for rsr_int4_matvec.
  */
 int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, const void *dout, int d_dtype, int act,

@@ -67,8 +67,8 @@ __global__ __launch_bounds__(256) void k_gated_slopes(const float *pre, const VT
 
 // ---- the transposed product ----------------------------------------------------------------------------
 // out[n][c] = sum over r of (dy[n][r] s[r][g]) (u[r][c] - (8 + z[r][g])), g the group of c.  The sum runs over the rows, so it is dy
-// that is scaled, once per group of columns, on its way into LDS (one bf16 plane, rounded, or three that hold all of
-// it); the codes are whole numbers as ever, and sum dy s (8 + z), the same for all columns of a group, is taken off at the end.
+// that is scaled, once per group of columns, on its way into LDS: as three bf16 planes, which hold all of it, or as two where dy and
+// out are both bf16 (one alone, dy s rounded to bf16, left results off by 0.0023 where rounding only them leaves 0.0017); the codes are whole numbers as ever, and sum dy s (8 + z), the same for all columns of a group, is taken off at the end.
 //
 // The matrix cores want eight consecutive rows of a column in a lane where the codes have eight columns of a row: they go
 // through LDS, where ds_read_b64_tr_b4 turns 16 rows of 16 nibbles around within 16 lanes.  Rows are laid out there as
@@ -103,29 +103,42 @@ __device__ __forceinline__ void widen_piece(const Piece<float> &p, float (&x)[8]
     for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(p.q[i >> 2][i & 3]);
 }
 
-// Eight rows of dy, scaled, to LDS; adds their sum times (8 + z), of what was written, to t: of three planes that of the top
-// one to t[0], of the others to t[1].  zeros: 8 + z in bf16, in the order that the rows are written in.
+// Eight rows of dy, scaled, to LDS as two or three planes of bf16; adds their sum times (8 + z), of what was written, to t: of three
+// planes that of the top one to t[0], of the others to t[1].  zeros: 8 + z in bf16, in the order that the rows are written in.
+// Two planes hold 16 bits: the product of a bf16 dy and a bf16 scale exactly, any other to 2^-16.
 template <int PLANES>
 __device__ __forceinline__ void stage_scaled(const float (&x)[8], const float (&scale)[8], u32x4 zeros, unsigned char *at,
                                              int plane, float (&t)[PLANES == 3 ? 2 : 1]) {
-    float y[8];
+    uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[i] * scale[i];
-    if constexpr (PLANES == 1) {
-        const u32x4 w = {rounded_pair(y[0], y[2]), rounded_pair(y[4], y[6]), rounded_pair(y[1], y[3]), rounded_pair(y[5], y[7])};
-        *reinterpret_cast<u32x4 *>(at) = w;
+    for (int i = 0; i < 8; ++i) {
+        const int r = i < 4 ? 2 * i : 2 * i - 7;
+        b[i] = __float_as_uint(x[r] * scale[r]);
+    }
+    auto tops = [&] { return u32x4{high_halves(b[0], b[1]), high_halves(b[2], b[3]), high_halves(b[4], b[5]), high_halves(b[6], b[7])}; };
+    if constexpr (PLANES == 2) {
+        const u32x4 top = tops();
+        u32x4 rest;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            t[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w[i]),
-                                                   __builtin_bit_cast(bf16x2, (uint32_t)zeros[i]), t[0], false);
+        for (int i = 0; i < 4; ++i) {
+            float y[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                y[e] = __uint_as_float(b[2 * i + e]) - __uint_as_float(b[2 * i + e] & 0xffff0000u);
+            rest[i] = rounded_pair(y[0], y[1]);
+        }
+        *reinterpret_cast<u32x4 *>(at) = top;
+        *reinterpret_cast<u32x4 *>(at + plane) = rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bf16x2 z = __builtin_bit_cast(bf16x2, (uint32_t)zeros[i]);
+            t[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)top[i]), z, t[0], false);
+            t[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)rest[i]), z, t[0], false);
+        }
     } else {
-        uint32_t b[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(y[i < 4 ? 2 * i : 2 * i - 7]);
 #pragma unroll
         for (int pl = 0; pl < 3; ++pl) {
-            *reinterpret_cast<u32x4 *>(at + pl * plane) =
-                u32x4{high_halves(b[0], b[1]), high_halves(b[2], b[3]), high_halves(b[4], b[5]), high_halves(b[6], b[7])};
+            *reinterpret_cast<u32x4 *>(at + pl * plane) = tops();
             if (pl < 2) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -133,7 +146,7 @@ __device__ __forceinline__ void stage_scaled(const float (&x)[8], const float (&
                     const float top = __uint_as_float(b[i] & 0xffff0000u), rest = __uint_as_float(b[i]) - top;
                     if (pl == 0) {
                         t[0] += top * z;
-                        t[PLANES == 3 ? 1 : 0] += rest * z;
+                        t[1] += rest * z;
                     }
                     b[i] = __float_as_uint(rest);
                 }
@@ -150,20 +163,21 @@ __device__ __forceinline__ void put_scale(float *scales, uint16_t *zeros, int at
 }
 
 // ---- tile: 128 columns --------------------------------------------------------------------------------
-// Two waves beside each other in columns, 64 each, and two in vectors, 32 VB each; KW = 2: two such sets, one multiplies the
+// Two waves beside each other in columns, 64 each, and two in vectors, 32 each; KW = 2: two such sets, one multiplies the
 // first eight rows of every row group and one the others, and they add up at the end.  A stage is ROWS rows of one matrix: dy
 // scaled for each of the NG groups of the 128 columns, and the codes.  One barrier per stage.
 // Three planes: the top one has sums of its own, whose products have few bits and add up almost exactly.
-// Scaling and rounding dy costs 25 vector instructions per eight elements and group of columns, whatever the tile, that is about
-// as long as the products of a group of 128; a tile of groups of 64 or 32 does it two or four times.  4096 x 14336, 2048 bf16
-// vectors, groups of 128: 317 us (759 TFLOP/s, a library product 191 to 216 us; per wave and stage of 64 rows 230 vector
-// instructions to 16 MFMAs, MFMA busy 35 %), of 64 437 us, of 32 789.  Not kept: the operands of a stage read before the
-// next one is written (334 us, and 355 instead of 302 for a training step of 6912 x 2560: its loads are asked for later), two stages of
-// loads on their way (336 and 343: more registers, fewer waves), three waves per SIMD enforced (no difference).
-template <typename VT, int PLANES, int NG, int VB, int ROWS, int KW>
+// Scaling dy and splitting it into planes costs 49 vector instructions per eight elements and group of columns (two planes; one
+// rounded plane took 25), about as long as the products of a group of 128; a tile of groups of 64 does it twice.  4096 x 14336, 2048 bf16
+// vectors, groups of 128: 531 us (453 TFLOP/s, twice that on the matrix cores; one rounded plane took 317), of 64 760 us.  Groups of
+// 32 have no tile: four scaled copies of a stage leave room for one workgroup per CU, 2151 us where split takes 1418.
+// Measured against it, groups of 128, two planes, 4096 x 14336, 2048 / 256 / 64 vectors: 64 rows in four waves 531 / 90 / 76 us, 128
+// rows in eight 664 / 100 / 53 (both are used), 64 rows in eight 635 / 93 / 63, 128 vectors with 32 rows in four 534 / 151 / 162, with 64
+// rows in eight 597 / 89 / 102, 32 rows in four 609 / 114 / 107.
+template <typename VT, int PLANES, int NG, int ROWS, int KW>
 struct BackTile {
     static constexpr int threads = 256 * KW;
-    static constexpr int vectors = 64 * VB;
+    static constexpr int vectors = 64;
     static constexpr int pieces = ROWS / 8;
     static constexpr int loads = vectors * pieces / threads;
     static constexpr int stride = ROWS * 2 + 16;  // bytes between vectors: an odd number of 16-byte units
@@ -179,13 +193,13 @@ struct BackTile {
     static constexpr int bytes = staged > joined ? staged : joined;
 };
 
-template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS, int KW>
+template <typename VT, typename OT, int PLANES, int NG, int ROWS, int KW>
 __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1, int both, int gpt,
                                                                const VT *__restrict__ dy, int ntiles, int n_rows,
                                                                int n_cols, long long ldv, int batch, float scale,
                                                                OT *__restrict__ out, long long ldo, int col_tiles,
                                                                int vec_tiles) {
-    using S = BackTile<VT, PLANES, NG, VB, ROWS, KW>;
+    using S = BackTile<VT, PLANES, NG, ROWS, KW>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wc = w & 1, wv = (w >> 1) & 1, kw = w >> 2;
@@ -281,7 +295,7 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
             }
         }
     };
-    f32x16 acc[S::sums][2][VB] = {};
+    f32x16 acc[S::sums][2] = {};
     request_scales(0);
     put_scales(0, 0);
     if (stages > 1) {
@@ -315,7 +329,7 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
         }
         request_scales(min(s + 3, stages - 1));
         const unsigned char *buf = smem + (s & 1) * S::buffer;
-        const unsigned char *operand = buf + (wv * 32 * VB + (lane & 31)) * S::stride + 32 * half;
+        const unsigned char *operand = buf + (wv * 32 + (lane & 31)) * S::stride + 32 * half;
         // lanes 0..15 and 16..31: the halves of a 32-column step, lanes from 32 on: the second row group
         const unsigned char *code = buf + S::codes + half * kCodeGroup + (lane & 15) * kCodeRow + 16 * (2 * wc) + 8 * ((lane >> 4) & 1);
 #pragma unroll
@@ -330,20 +344,15 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
                 for (int r = 0; r < 2; ++r) x[r] = decode((uint32_t)(KW == 1 ? y[r][mm] : kw ? y[r].y : y[r].x));
                 const unsigned char *at_m = operand + 64 * q + 16 * (KW == 1 ? mm : kw);
 #pragma unroll
-                for (int n = 0; n < VB; ++n)
+                for (int pl = 0; pl < PLANES; ++pl) {
+                    // (one group of all 128 columns, or one per wave)
+                    const bf16x8 o = lds_operand(at_m + pl * S::plane + (NG == 1 ? 0 : wc) * S::copy);
 #pragma unroll
-                    for (int pl = 0; pl < PLANES; ++pl) {
-                        const unsigned char *at = at_m + pl * S::plane + n * 32 * S::stride;
-                        bf16x8 o[2];
-                        // (groups of this wave's two 32-column steps: one of all 128 columns, one per 64, one per 32)
-                        o[0] = lds_operand(at + (NG == 1 ? 0 : NG == 2 ? wc : 2 * wc) * S::copy);
-                        o[1] = NG == 4 ? lds_operand(at + (2 * wc + 1) * S::copy) : o[0];
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            f32x16 &to = acc[pl ? S::sums - 1 : 0][r][n];
-                            to = mfma32(o[r], x[r], to);
-                        }
+                    for (int r = 0; r < 2; ++r) {
+                        f32x16 &to = acc[pl ? S::sums - 1 : 0][r];
+                        to = mfma32(o, x[r], to);
                     }
+                }
             }
         }
         __syncthreads();
@@ -358,26 +367,21 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
     __builtin_amdgcn_s_waitcnt(0x0f70);
     if constexpr (S::sums == 2) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int n = 0; n < VB; ++n) acc[0][r][n] += acc[1][r][n];
+        for (int r = 0; r < 2; ++r) acc[0][r] += acc[1][r];
     }
     if constexpr (KW == 2) {
-        // the second set hands over its sums, 32 registers at a time (the last barrier is behind every read of the buffers)
+        // the second set hands over its sums (the last barrier is behind every read of the buffers)
         float *red = reinterpret_cast<float *>(smem) + (w & 3) * 2048 + lane;
+        if (kw == 1) {
 #pragma unroll
-        for (int n = 0; n < VB; ++n) {
-            if (kw == 1) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) red[i * 64] = acc[0][i >> 4][n][i & 15];
-            }
-            __syncthreads();
-            if (kw == 0) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) acc[0][i >> 4][n][i & 15] += red[i * 64];
-            }
-            __syncthreads();
+            for (int i = 0; i < 32; ++i) red[i * 64] = acc[0][i >> 4][i & 15];
         }
+        __syncthreads();
+        if (kw == 0) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[0][i >> 4][i & 15] += red[i * 64];
+        }
+        __syncthreads();
     }
     // what is taken off, per group and vector
     float *off = reinterpret_cast<float *>(smem);
@@ -394,22 +398,21 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int col = ct * 128 + wc * 64 + r * 32 + turned_column(lane & 31);
-        const float *o = off + (NG == 1 ? 0 : NG == 2 ? wc : 2 * wc + r) * S::vectors;
+        const float *o = off + (NG == 1 ? 0 : wc) * S::vectors;
 #pragma unroll
-        for (int n = 0; n < VB; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int v = (wv * VB + n) * 32 + acc_row(i, half);
-                if (vec0 + v < batch && col < n_cols)
-                    put(out + (long long)(vec0 + v) * ldo + col, scale * (acc[0][r][n][i] - o[v]));
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int v = wv * 32 + acc_row(i, half);
+            if (vec0 + v < batch && col < n_cols)
+                put(out + (long long)(vec0 + v) * ldo + col, scale * (acc[0][r][i] - o[v]));
+        }
     }
 }
 
 // ---- split: up to 32 vectors -----------------------------------------------------------------------------
 // WAVES waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.  Bound by the chain
-// of a step (scales, dy, operands: three turns through LDS) and what is around it: 4096 x 14336, one bf16 vector 13.7 us (2.2 TB/s,
-// a plain read of the codes 6.2), where branches around its requests had all loads waited for 22.5.
+// of a step (scales, dy, operands: three turns through LDS) and what is around it: 4096 x 14336, one bf16 vector 17.2 us (1.7 TB/s,
+// a plain read of the codes 6.2; 13.7 with dy s rounded to one plane, and that 22.5 where branches around its requests had all loads
+// waited for).
 // Up to 16 vectors (VECS): the other 16 rows of the MFMA repeat them.
 template <int PLANES, int NG, int VECS>
 struct BackSplit {
@@ -592,11 +595,11 @@ struct Args {
     hipStream_t stream;
 };
 
-template <typename VT, typename OT, int PLANES, int NG, int VB, int ROWS, int KW>
+template <typename VT, typename OT, int PLANES, int NG, int ROWS, int KW>
 hipError_t launch_tile(const Args &x) {
-    using S = BackTile<VT, PLANES, NG, VB, ROWS, KW>;
+    using S = BackTile<VT, PLANES, NG, ROWS, KW>;
     static std::atomic<size_t> enabled[kMaxDevices];
-    auto kern = k_int4_back_tile<VT, OT, PLANES, NG, VB, ROWS, KW>;
+    auto kern = k_int4_back_tile<VT, OT, PLANES, NG, ROWS, KW>;
     static_assert(S::bytes <= kLdsBytes && S::codes >= NG * S::vectors * 4, "two stages, and then what is taken off");
     if (hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kern), S::bytes, x.device, enabled)) return e;
     const int col_tiles = (x.n_cols + 127) / 128, vec_tiles = (x.batch + S::vectors - 1) / S::vectors;
@@ -626,47 +629,50 @@ hipError_t launch_split_waves(const Args &x) {
 template <typename VT, typename OT, int PLANES, int NG>
 hipError_t launch_split(const Args &x) {
     if (x.batch > 16) return launch_split_waves<VT, OT, PLANES, NG, 32, 8>(x);
-    // sixteen waves where every one gets two steps, and the registers allow it
-    if constexpr (PLANES == 1 && sizeof(VT) == 2)
-        if (x.n_rows >= 1024) return launch_split_waves<VT, OT, PLANES, NG, 16, 16>(x);
+    // sixteen waves where every one gets four steps, and the registers allow it.  Measured, one vector, sixteen / eight: 14336 x 4096
+    // 38.5 / 47.2 us, 4096 x 14336 17.3 / 18.3, 2560 x 6912 in groups of 32 13.1 / 14.2, 1024 x 1024 in groups of 32 7.5 / 7.2
+    if constexpr (PLANES == 2 && sizeof(VT) == 2)
+        if (x.n_rows >= 2048) return launch_split_waves<VT, OT, PLANES, NG, 16, 16>(x);
     return launch_split_waves<VT, OT, PLANES, NG, 16, 8>(x);
 }
 
-// Estimates in microseconds.  A wave of split takes 0.92 us (three planes 1.4) per 32 rows, a workgroup of a tile about as
-// long per stage whatever its shape, and rounds of more workgroups than the chip runs at once follow one another.  Measured for groups of
-// 128 columns, split / tiles of 64 vectors / of 128: bf16 14336 x 4096, 64 vectors 46 / 124 / 343, 256 vectors 89 / 122 / 290; 4096 x
-// 14336, 64 vectors 32 / 41 / 106, 256 104 / 60 / 90, 2048 - / 399 / 317; 6912 x 2560, 256 46 / 64 / 145, 512 68 / 63, 2048 - / 140 / 157; 2560 x 6912, 256 43 / 29 /
-// 60; 640 x 2560, 128 6.7 / 11 / 19; float32 4096 x 14336, 40 vectors 48 / 98, 100 vectors 94 / 92.  Two workgroups of eight waves do
-// not fit a CU together, but the CUs that finish early take up to a quarter of a round more at little cost, hence 320 for 256 CUs.
-float rounds_of(int columns, int vectors, const Args &x, int at_once) {
-    const float groups = (float)((x.n_cols + columns - 1) / columns) * (float)((x.batch + vectors - 1) / vectors);
-    return groups <= (float)at_once ? 1.0f : groups / (float)at_once;
-}
-float tile_us(const Args &x, int rows, int vectors, float stage_us, int at_once) {
-    return 3.0f + stage_us * (float)((x.n_rows + rows - 1) / rows) * (x.both ? 2.0f : 1.0f) * rounds_of(128, vectors, x, at_once);
+// Estimates in microseconds for more than 32 vectors.  A round of split, one workgroup per CU, takes 1.12 us (three planes 1.4) per 256
+// rows.  A workgroup of a tile takes 1.1 us per 64 rows and 1.46 per 128 (two planes), 1.15 per 64 (three); those of 128 rows, and of
+// three planes, have a CU to themselves and go in rounds, the others share it, three at once, for 0.58 us more each.  Measured, split / 128 rows /
+// 64 rows, groups of 128, two planes: 4096 x 14336, 64 vectors 43 / 53 / 76, 256 136 / 100 / 90, 2048 1040 / 664 / 531; 14336 x 4096, 256
+// vectors 132 / 161 / 245, 2048 911 / 636 / 582; 6912 x 2560, 256 60 / 82 / 115, 512 91 / 80 / 114, 2048 299 / 230 / 199; 2560 x 6912, 64
+// 15 / 35 / 47, 256 56 / 36 / 47; both matrices of 6912 x 2560, 1024 vectors 304 / 317 / 299.  Three planes, split / tile: 4096 x 14336,
+// 64 54 / 80, 256 171 / 150; 14336 x 4096, 256 161 / 257, 512 304 / 257.
+// Groups of 64, two planes, split / tile (32 rows): 4096 x 14336, 128 vectors 78 / 127, 512 264 / 257, 2048 1041 / 760; 14336 x 4096, 1024
+// 494 / 465.  In groups of 64 tiles of three planes lose to split (4096 x 14336, 256 and 512 vectors 174 / 182 and 336 / 366; 6912 x 2560,
+// 512 117 / 260), in groups of 32 all do (three planes: 230 / 414 and 451 / 826; two: 128 and 2048 vectors 103 / 170 and 1418 / 2151).
+float per_cu(int columns, int vectors, const Args &x) {
+    return (float)((((long long)x.n_cols + columns - 1) / columns * ((x.batch + vectors - 1) / vectors) + 255) / 256);
 }
 
 template <typename VT, typename OT, int PLANES>
 hipError_t launch_all(const Args &x) {
-    constexpr bool one = PLANES == 1;
-    const float split = 4.0f + (one ? 0.92f : 1.4f) * (float)x.n_rows / 256.0f * (x.both ? 2.0f : 1.0f) * rounds_of(64, 32, x, 256);
-    const bool few = x.batch <= 32;
-    if (x.gpt == 8) {
-        if (few || split < tile_us(x, 32, 64, 1.0f, 512)) return launch_split<VT, OT, PLANES, 2>(x);
-        return launch_tile<VT, OT, PLANES, 4, 1, 32, 1>(x);
+    if (x.gpt == 8) return launch_split<VT, OT, PLANES, 2>(x);
+    if (x.batch <= 32 || (x.gpt == 4 && PLANES == 3)) return launch_split<VT, OT, PLANES, 1>(x);
+    const float rows = (float)x.n_rows * (x.both ? 2.0f : 1.0f), tiles = per_cu(128, 64, x);
+    const float split = 4.0f + (PLANES == 3 ? 1.4f : 1.12f) * rows / 256.0f * per_cu(64, 32, x);
+    auto shared = [&](int stage_rows, float alone, float more) {
+        const float together = 0.2f + more * tiles;
+        return 3.0f + rows / (float)stage_rows * (alone > together ? alone : together);
+    };
+    if constexpr (PLANES == 3) {
+        if (split < 3.0f + 1.15f * rows / 64.0f * tiles) return launch_split<VT, OT, PLANES, 1>(x);
+        return launch_tile<VT, OT, PLANES, 1, 64, 2>(x);
+    } else {
+        if (x.gpt == 4) {
+            if (split < shared(32, 0.97f, 0.42f)) return launch_split<VT, OT, PLANES, 1>(x);
+            return launch_tile<VT, OT, PLANES, 2, 32, 1>(x);
+        }
+        const float few = 3.0f + 1.46f * rows / 128.0f * tiles, many = shared(64, 1.1f, 0.58f);
+        if (split < (few < many ? few : many)) return launch_split<VT, OT, PLANES, 1>(x);
+        if (many < few) return launch_tile<VT, OT, PLANES, 1, 64, 1>(x);
+        return launch_tile<VT, OT, PLANES, 1, 128, 2>(x);
     }
-    if (x.gpt == 4) {
-        constexpr int rows = one ? 64 : 32;
-        if (few || split < tile_us(x, rows, 64, 1.2f, 512)) return launch_split<VT, OT, PLANES, 1>(x);
-        return launch_tile<VT, OT, PLANES, 2, 1, rows, 1>(x);
-    }
-    constexpr int rows = one ? 128 : 64;
-    const float small = tile_us(x, rows, 64, one ? 1.1f : 1.4f, one ? 320 : 256);
-    const float large = one ? tile_us(x, 64, 128, 1.35f, 512) : small;
-    if (few || split < (small < large ? small : large)) return launch_split<VT, OT, PLANES, 1>(x);
-    if constexpr (one)
-        if (large < small) return launch_tile<VT, OT, 1, 1, 2, 64, 1>(x);
-    return launch_tile<VT, OT, PLANES, 1, 1, rows, 2>(x);
 }
 
 // (A launch holds fewer than 2^32 threads, at most 1024 per 64 columns and 32 vectors, and 65535 sets of vectors: so many at
@@ -688,7 +694,7 @@ hipError_t launch(const Args &x) {
 
 }  // namespace
 
-hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool rounded,
+hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool short_dy,
                                   float scale, void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo,
                                   hipStream_t stream) {
     Args x = {};
@@ -708,9 +714,9 @@ hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, 
     x.out = out;
     x.stream = stream;
     if (v_dtype == RSR_BF16)
-        return out_dtype != RSR_BF16 ? launch<uint16_t, float, 3>(x) : launch<uint16_t, uint16_t, 1>(x);
+        return out_dtype != RSR_BF16 ? launch<uint16_t, float, 3>(x) : launch<uint16_t, uint16_t, 2>(x);
     if (out_dtype != RSR_BF16) return launch<float, float, 3>(x);
-    return rounded ? launch<float, uint16_t, 1>(x) : launch<float, uint16_t, 3>(x);
+    return short_dy ? launch<float, uint16_t, 2>(x) : launch<float, uint16_t, 3>(x);
 }
 
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,

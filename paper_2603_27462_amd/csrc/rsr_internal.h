@@ -187,9 +187,9 @@ void int4_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, 
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,
                              void *out, int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo,
                              hipStream_t stream);
-// out[n] = scale * (a^T dy[n] + b^T dy[n] further on by a's rows); b may be null.  rounded: for a bf16 result dy, scaled, is
-// rounded to bf16 (it always is where dy is bf16 as well).
-hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool rounded,
+// out[n] = scale * (a^T dy[n] + b^T dy[n] further on by a's rows); b may be null.  short_dy: for a bf16 result dy, scaled, is
+// kept to 16 bits (it always is where dy is bf16 as well: the product of two bf16 has no more).
+hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool short_dy,
                                   float scale, void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo,
                                   hipStream_t stream);
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,
