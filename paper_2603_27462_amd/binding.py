@@ -172,6 +172,21 @@ def _stream_ptr(stream) -> int:
     return _raw_stream(_current_device())
 
 
+def _new(shape, dtype, device, stream):
+    """A new tensor for what a call on `stream` writes (None: the current one).  Allocated on that stream: memory that was freed
+    on the current one may be in use there until its work ends, which a kernel on another stream does not wait for.  The
+    caller's program is expected to go on with it on the current stream, so it is kept for that one too."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    out.record_stream(torch.cuda.current_stream(device))
+    return out
+
+
 def _raw_stream(device: int) -> int:
     """Pointer of torch's current stream on `device`; replaced on its first call by torch's own
     function where this torch has it."""
@@ -253,7 +268,7 @@ def rsr_matvec_stacked(h: Handle, v, scales=None, outs=None, stream=None):
     if not (v.is_cuda and v.dim() == 1 and v.numel() == h.cols and v.is_contiguous()):
         raise TypeError("v must be a contiguous CUDA vector of length cols")
     if outs is None:
-        outs = [torch.empty(r, dtype=torch.float32, device=v.device) for r in h.layer_rows]
+        outs = [_new(r, torch.float32, v.device, stream) for r in h.layer_rows]
     optr = (ctypes.c_void_p * n)(*[o.data_ptr() for o in outs])
     sc = (ctypes.c_float * n)(*[float(x) for x in scales]) if scales is not None else None
     rc = load_library().rsr_matvec_stacked(h.ptr, v.data_ptr(), _dtype_code(v), sc, optr, _stream_ptr(stream))
@@ -323,7 +338,7 @@ def rsr_matvec(h: Handle, v, out=None, stream=None):
     if not (v.is_cuda and v.dtype == torch.float32 and v.is_contiguous() and v.numel() == h.cols):
         raise TypeError("v must be a contiguous float32 CUDA tensor of length cols")
     if out is None:
-        out = torch.empty(h.rows, dtype=torch.float32, device=v.device)
+        out = _new(h.rows, torch.float32, v.device, stream)
     rc = load_library().rsr_matvec(h.ptr, v.data_ptr(), out.data_ptr(), _stream_ptr(stream))
     if rc:
         raise RsrError(rc, "rsr_matvec")
@@ -343,14 +358,14 @@ def rsr_matvec_ex(h: Handle, v, scale: float = 1.0, out=None, stream=None):
             raise TypeError(_VECTORS)
         batch, ldv = 1, h.cols
         if out is None:
-            out = torch.empty(h.rows, dtype=torch.float32, device=v.device)
+            out = _new(h.rows, torch.float32, v.device, stream)
     elif dim == 2:
         batch, cols = v.shape
         ldv, inner = v.stride()
         if cols != h.cols or inner != 1:
             raise TypeError(_VECTORS)
         if out is None:
-            out = torch.empty((batch, h.rows), dtype=torch.float32, device=v.device)
+            out = _new((batch, h.rows), torch.float32, v.device, stream)
     else:
         raise TypeError(_VECTORS)
     ldo = h.rows if out.dim() == 1 else out.stride(0)
@@ -413,12 +428,12 @@ def _vectors(v, length: int, device, name: str):
     return batch, length if batch <= 1 else v.stride(0), _dtype_code(v)
 
 
-def _result(out, like, length: int, dtype, name: str = "out"):
-    """`out`, checked against the vectors `like`, or a new tensor for their results."""
+def _result(out, like, length: int, dtype, stream, name: str = "out"):
+    """`out`, checked against the vectors `like`, or a new tensor for their results, which a call on `stream` writes."""
     import torch
     shape = (*like.shape[:-1], length)
     if out is None:
-        return torch.empty(shape, dtype=dtype or torch.float32, device=like.device)
+        return _new(shape, dtype or torch.float32, like.device, stream)
     if (tuple(out.shape) != shape or out.device != like.device or (length > 1 and out.stride(-1) != 1) or
             out.dtype not in (torch.float32, torch.bfloat16) or (dtype is not None and out.dtype != dtype)):
         raise TypeError("%s must be a float32 or bfloat16 tensor %s with unit inner stride on the handle's device, of the type "
@@ -452,7 +467,7 @@ def rsr_int4_matvec(h: Handle, v, transposed: bool = False, scale: float = 1.0, 
     device = _int4_device(h)
     length, to = (h.rows, h.cols) if transposed else (h.cols, h.rows)
     batch, ldv, code = _vectors(v, length, device, "v")
-    out = _result(out, v, to, dtype)
+    out = _result(out, v, to, dtype, stream)
     ldo = to if batch <= 1 else out.stride(0)
     rc = _on(device, stream, lambda s: load_library().rsr_int4_matvec(
         h.ptr, int(bool(transposed)), v.data_ptr(), code, float(scale), out.data_ptr(), _dtype_code(out), batch, ldv, ldo,
@@ -481,7 +496,7 @@ def rsr_gated(gate: Handle, up: Handle, v, act="silu", dtype=None, out=None, pre
             return out
     device = _int4_device(gate, up)
     batch, ldv, code = _vectors(v, gate.cols, device, "v")
-    out = _result(out, v, gate.rows, dtype)
+    out = _result(out, v, gate.rows, dtype, stream)
     if pre is not None:
         _kept(pre, batch, gate.rows, device, "pre")
     ldo = gate.rows if batch <= 1 else out.stride(0)
@@ -498,15 +513,14 @@ def rsr_gated_backward(gate: Handle, up: Handle, pre, dout, act="silu", dtype=No
     """(dv, dpre) of rsr_gated for the gradient dout of its result and the `pre` it wrote: dv [batch][cols] of type `dtype`, by
     default float32 (None without need_dv), and dpre, float32 [batch][2][rows], the gradients of both products; a dpre given
     may be `pre` itself."""
-    import torch
     device = _int4_device(gate, up)
     batch, ldd, code = _vectors(dout, gate.rows, device, "dout")
     _kept(pre, batch, gate.rows, device, "pre")
     if dpre is None:
-        dpre = torch.empty_like(pre)
+        dpre = _new(pre.shape, pre.dtype, pre.device, stream)
     _kept(dpre, batch, gate.rows, device, "dpre")
     if need_dv:
-        dv = _result(dv, dout, gate.cols, dtype, "dv")
+        dv = _result(dv, dout, gate.cols, dtype, stream, "dv")
     else:
         dv = None
     lddv = gate.cols if batch <= 1 or dv is None else dv.stride(0)
