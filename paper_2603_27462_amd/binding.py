@@ -390,6 +390,8 @@ def rsr_preprocess_int4(Q, scales, group: int, zeros=None) -> Handle:
     rows, cols = Q.shape
     group = int(group)
     shape = (rows, -(-cols // group) if group > 0 else 0)
+    if group > cols > 0:
+        group = cols    # one scale per row, as any number beyond; the library's argument has 64 bits and would wrap
     if not (isinstance(scales, torch.Tensor) and scales.device == Q.device and tuple(scales.shape) == shape and
             scales.dtype in (torch.float32, torch.bfloat16, torch.float16)):
         raise TypeError("scales must be a float tensor [rows][ceil(cols / group)] on the device of Q")
