@@ -41,7 +41,7 @@ class RsrError(RuntimeError):
 
 _lib = None
 _product = None     # rsr_call.cpp: rsr_matvec_ex with a new result on the current stream, or None if it is not built
-_int4 = _gated = None   # the same of rsr_int4_matvec and rsr_gated
+_int4 = _gated = None   # the same of rsr_int4_matvec and rsr_gated: used where _product is
 
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
@@ -129,7 +129,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
 
 def _load_call(lib) -> None:
     global _product, _int4, _gated
-    _product = _int4 = _gated = None
+    _product = None
     try:
         loader = importlib.machinery.ExtensionFileLoader("_rsr_call", _build.CALL_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_rsr_call", loader))
@@ -462,7 +462,7 @@ def _on(device, stream, call) -> int:
 def rsr_int4_matvec(h: Handle, v, transposed: bool = False, scale: float = 1.0, dtype=None, out=None, stream=None):
     """scale * M v, or scale * M^T v: v [length] or [batch][length], float32 or bfloat16, length cols (transposed: rows).
     The result is of type `dtype`, by default float32."""
-    if out is None and stream is None and _int4 is not None and dtype in _RESULTS:
+    if out is None and stream is None and _product is not None and dtype in _RESULTS:
         out = _int4(h.ptr, h.rows, h.cols, v, transposed, scale, _RESULTS[dtype])
         if out is not None:
             return out
@@ -492,7 +492,7 @@ def rsr_gated(gate: Handle, up: Handle, v, act="silu", dtype=None, out=None, pre
     is of type `dtype`, by default float32.  pre: a float32 tensor [batch][2][rows] that receives both products, for
     rsr_gated_backward."""
     act = _act_code(act)
-    if out is None and pre is None and stream is None and _gated is not None and dtype in _RESULTS:
+    if out is None and pre is None and stream is None and _product is not None and dtype in _RESULTS:
         out = _gated(gate.ptr, up.ptr, gate.rows, gate.cols, v, act, _RESULTS[dtype])
         if out is not None:
             return out
