@@ -1,11 +1,12 @@
 """Torch modules around handles (the role the paper gives its RSRLinear layer in System Overview, "Integration": a
 drop-in for a linear layer whose weight is fixed after preprocessing): RsrLinear for binary and ternary weights, RsrInt4Linear
 for 4-bit weights with group scales, and RsrGatedMlp, the feed-forward block of three of those.  The latter two pass gradients on
-to their inputs, so that what lies before and beside them can be trained.  Argument marshalling only: the products run
+to their inputs, so that what lies before and beside them can be trained (in reverse mode, once; forward mode is refused).  Argument marshalling only: the products run
 in librsr."""
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding as _b
@@ -54,7 +55,18 @@ def _rows(x: torch.Tensor, length: int) -> torch.Tensor:
     return flat if whole else flat.contiguous()
 
 
-class _Int4Product(torch.autograd.Function):
+def _differentiated(x: torch.Tensor) -> bool:
+    """whether a derivative of x is asked for, in reverse mode or (refused below) in forward mode"""
+    return (torch.is_grad_enabled() and x.requires_grad) or forward_ad.unpack_dual(x).tangent is not None
+
+
+class _ReverseMode(torch.autograd.Function):
+    @staticmethod
+    def jvp(ctx, *tangents):
+        raise NotImplementedError("layers of 4-bit weights pass gradients on in reverse mode only")
+
+
+class _Int4Product(_ReverseMode):
     @staticmethod
     def forward(ctx, x, handle, dtype):
         ctx.handle, ctx.dtype = handle, x.dtype
@@ -67,7 +79,7 @@ class _Int4Product(torch.autograd.Function):
         return dx, None, None
 
 
-class _Gated(torch.autograd.Function):
+class _Gated(_ReverseMode):
     @staticmethod
     def forward(ctx, x, gate, up, act):
         pre = torch.empty((x.shape[0], 2, gate.rows), dtype=torch.float32, device=x.device)
@@ -96,7 +108,7 @@ class RsrInt4Linear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         flat = _rows(x, self.in_features)
-        if torch.is_grad_enabled() and x.requires_grad:
+        if _differentiated(x):
             y = _Int4Product.apply(flat, self.handle, self.dtype)
         else:
             y = _b.rsr_int4_matvec(self.handle, flat.detach(), dtype=self.dtype)
@@ -119,7 +131,7 @@ class RsrGatedMlp(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         flat = _rows(x, self.gate.in_features)
-        if torch.is_grad_enabled() and x.requires_grad:
+        if _differentiated(x):
             h = _Gated.apply(flat, self.gate.handle, self.up.handle, self.act)
         else:
             h = _b.rsr_gated(self.gate.handle, self.up.handle, flat.detach(), self.act, dtype=flat.dtype)
