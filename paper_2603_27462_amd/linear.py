@@ -114,6 +114,12 @@ class RsrInt4Linear(torch.nn.Module):
             y = _b.rsr_int4_matvec(self.handle, flat.detach(), dtype=self.dtype)
         return y.reshape(*x.shape[:-1], self.out_features)
 
+    def kept_group(self) -> int:
+        """columns of a group as the handle keeps them"""
+        if self.group >= self.in_features:
+            return 128
+        return next(n for n in (128, 64, 32) if self.group % n == 0)
+
     def extra_repr(self) -> str:
         return "in_features=%d, out_features=%d, group=%d" % (self.in_features, self.out_features, self.group)
 
@@ -126,6 +132,11 @@ class RsrGatedMlp(torch.nn.Module):
         super().__init__()
         if (gate.in_features, gate.out_features) != (up.in_features, up.out_features) or down.in_features != gate.out_features:
             raise ValueError("gate and up must have one shape, and down the inputs that they have outputs")
+        if gate.kept_group() != up.kept_group():
+            raise ValueError("the groups of gate and up must be multiples of the same of 32, 64 and 128 (%d and %d are kept as %d and %d)"
+                             % (gate.group, up.group, gate.kept_group(), up.kept_group()))
+        if not gate.handle.device == up.handle.device == down.handle.device:
+            raise ValueError("gate, up and down must be on one device")
         _b._act_code(act)
         self.gate, self.up, self.down, self.act = gate, up, down, act
 

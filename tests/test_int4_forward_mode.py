@@ -13,7 +13,7 @@ class _Weight:
     def __init__(self, codes, scales, group, zeros=None):
         self.rows, self.cols = codes.shape
         self.matrix = codes.float() * scales.repeat_interleave(group, dim=1)[:, :self.cols]
-        self.group = group
+        self.device = scales.device
 
 
 def _matvec(h, v, transposed=False, scale=1.0, dtype=None, out=None, stream=None):
