@@ -315,6 +315,13 @@ int rsr_gated(rsr_handle_t gate, rsr_handle_t up, const void *v, int v_dtype, in
 int rsr_gated_backward(rsr_handle_t gate, rsr_handle_t up, const float *pre, const void *dout, int d_dtype, int act,
                        float *dpre, void *dv, int dv_dtype, int batch, int64_t ldd, int64_t lddv, void *stream);
 
+/*
+ * rsr_int4_kernel_name -- the kernel that rsr_int4_matvec launches for `batch` vectors of these types, as a profiler reports it
+ * (of several launches the first).  With `up`: that of rsr_gated, and with `transposed` too the product of
+ * rsr_gated_backward, whose vectors are float32 (RSR_EINVAL for another v_dtype).  Valid until the thread's next call; NULL on error.
+ */
+const char *rsr_int4_kernel_name(rsr_handle_t h, rsr_handle_t up, int transposed, int v_dtype, int out_dtype, int batch);
+
 /* Frees the handle and its device buffers.  NULL is allowed. */
 void rsr_destroy(rsr_handle_t h);
 

@@ -13,5 +13,5 @@ from .binding import (  # noqa: F401
     rsr_num_blocks, rsr_block_height, rsr_num_patterns, rsr_num_passes, rsr_algorithmic_bytes,
     rsr_kernel_name, rsr_launch_shape, rsr_probe_empty, rsr_probe_read,
     rsr_preprocess_stacked, rsr_matvec_stacked, rsr_batch_kernel_name,
-    rsr_preprocess_int4, rsr_int4_matvec, rsr_gated, rsr_gated_backward,
+    rsr_preprocess_int4, rsr_int4_matvec, rsr_gated, rsr_gated_backward, rsr_int4_kernel_name,
 )

@@ -29,7 +29,7 @@ exported_symbols = [
     "rsr_algorithmic_bytes",
     "rsr_kernel_name", "rsr_preprocess_into", "rsr_launch_shape", "rsr_probe_empty", "rsr_probe_read",
     "rsr_preprocess_stacked", "rsr_matvec_stacked", "rsr_num_layers", "rsr_batch_kernel_name",
-    "rsr_preprocess_int4", "rsr_int4_matvec", "rsr_gated", "rsr_gated_backward",
+    "rsr_preprocess_int4", "rsr_int4_matvec", "rsr_gated", "rsr_gated_backward", "rsr_int4_kernel_name",
 ]
 
 
@@ -122,6 +122,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.rsr_gated.argtypes = [vp, vp, vp, ci, ci, vp, ci, vp, ci, i64, i64, vp]
     lib.rsr_gated_backward.restype = ci
     lib.rsr_gated_backward.argtypes = [vp, vp, vp, vp, ci, ci, vp, vp, ci, ci, i64, i64, vp]
+    lib.rsr_int4_kernel_name.restype = ctypes.c_char_p
+    lib.rsr_int4_kernel_name.argtypes = [vp, vp, ci, ci, ci, ci]
     _lib = lib
     _load_call(lib)
     return lib
@@ -533,6 +535,15 @@ def rsr_gated_backward(gate: Handle, up: Handle, pre, dout, act="silu", dtype=No
     if rc:
         raise RsrError(rc, "rsr_gated_backward")
     return dv, dpre
+
+
+def rsr_int4_kernel_name(h: Handle, up: Optional[Handle] = None, transposed: bool = False, v_dtype: int = RSR_F32,
+                         out_dtype: int = RSR_F32, batch: int = 1) -> str:
+    """The kernel of rsr_int4_matvec, with `up` that of rsr_gated, with both the product's of rsr_gated_backward."""
+    s = load_library().rsr_int4_kernel_name(h.ptr, None if up is None else up.ptr, int(bool(transposed)), v_dtype, out_dtype, int(batch))
+    if s is None:
+        raise RsrError(rsr_last_error(), "rsr_int4_kernel_name")
+    return s.decode()
 
 
 _VECTORS = "v must be a CUDA tensor [cols] or [batch][cols] with unit inner stride"

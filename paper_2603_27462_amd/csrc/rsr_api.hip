@@ -1141,13 +1141,29 @@ const char *rsr_batch_kernel_name(rsr_handle_t h, int v_dtype, int batch) {
     }
     static thread_local char name[96];
     if (h->kind == RSR_INT4)
-        rsr::int4_kernel_name(h, v_dtype, batch, name, sizeof(name));
+        rsr::int4_kernel_name(h, nullptr, v_dtype, batch, name, sizeof(name));
     else if (use_packed(h, v_dtype, batch, h->cols * (v_dtype == RSR_BF16 ? 2 : 4) % 16 == 0))
         rsr::packed_kernel_name(h, v_dtype, batch, name, sizeof(name));
     else if (h->narrow)
         return v_dtype == RSR_BF16 ? "k_rsr_narrow<unsigned short>" : "k_rsr_narrow<float>";
     else
         rsr::rsr_matvec_kernel_name(h, v_dtype, batch, name, sizeof(name));
+    return name;
+}
+
+const char *rsr_int4_kernel_name(rsr_handle_t h, rsr_handle_t up, int transposed, int v_dtype, int out_dtype, int batch) {
+    int rc = is_int4(h) && vector_type(v_dtype) && vector_type(out_dtype) && batch >= 1 ? RSR_OK : RSR_EINVAL;
+    if (rc == RSR_OK && up) rc = transposed && v_dtype != RSR_F32 ? RSR_EINVAL : check_pair(h, up, RSR_SILU);
+    if (rc == RSR_OK && batch > rsr::kInt4MaxBatch) rc = RSR_EUNSUPPORTED;
+    if (rc != RSR_OK) {
+        fail(rc);
+        return nullptr;
+    }
+    static thread_local char name[96];
+    if (transposed)
+        rsr::int4_transposed_kernel_name(h, up, v_dtype, up != nullptr, out_dtype, batch, name, sizeof(name));
+    else
+        rsr::int4_kernel_name(h, up, v_dtype, batch, name, sizeof(name));
     return name;
 }
 

@@ -705,6 +705,7 @@ struct Args {
 
 template <typename VT, typename... Number>
 hipError_t put_name(const Args &x, const char *kernel, const char *numbers, Number... n) {
+    if (x.name[0]) return hipSuccess;  // (of several launches the first)
     const int at = std::snprintf(x.name, x.name_len, "%s<%s, ", kernel, sizeof(VT) == 4 ? "float" : "unsigned short");
     if (at > 0 && (size_t)at < x.name_len) std::snprintf(x.name + at, x.name_len - at, numbers, n...);
     return hipSuccess;
@@ -870,11 +871,15 @@ hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float 
     return v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group);
 }
 
-void int4_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len) {
-    Args x = args_of(h, nullptr, 0, nullptr, 1.0f, nullptr, RSR_F32, nullptr, batch, h->cols, h->rows, nullptr);
+void int4_kernel_name(const rsr_handle_s *h, const rsr_handle_s *up, int v_dtype, int batch, char *buf, size_t len) {
+    Args x = args_of(h, up, 0, nullptr, 1.0f, nullptr, RSR_F32, nullptr, batch, h->cols, h->rows, nullptr);
     x.name = buf;
     x.name_len = len;
-    (void)(v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group));
+    buf[0] = 0;
+    if (up)
+        (void)(v_dtype == RSR_BF16 ? launch_groups<uint16_t, 2>(x, h->group) : launch_groups<float, 2>(x, h->group));
+    else
+        (void)(v_dtype == RSR_BF16 ? launch_groups<uint16_t, 1>(x, h->group) : launch_groups<float, 1>(x, h->group));
 }
 
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,

@@ -2,6 +2,7 @@
 // gated block's activation.
 #include "rsr_int4.h"
 
+#include <cstdio>
 #include <type_traits>
 
 namespace rsr {
@@ -593,11 +594,21 @@ struct Args {
     float scale;
     void *out;
     hipStream_t stream;
+    char *name;  // not null: write the name of the kernel there (of several the first) instead of launching it
+    size_t name_len;
 };
+
+template <typename VT, typename OT, typename... Number>
+hipError_t put_name(const Args &x, const char *format, Number... n) {
+    if (!x.name[0])
+        std::snprintf(x.name, x.name_len, format, sizeof(VT) == 4 ? "float" : "unsigned short", sizeof(OT) == 4 ? "float" : "unsigned short", n...);
+    return hipSuccess;
+}
 
 template <typename VT, typename OT, int PLANES, int NG, int ROWS, int KW>
 hipError_t launch_tile(const Args &x) {
     using S = BackTile<VT, PLANES, NG, ROWS, KW>;
+    if (x.name) return put_name<VT, OT>(x, "k_int4_back_tile<%s, %s, %d, %d, %d, %d>", PLANES, NG, ROWS, KW);
     static std::atomic<size_t> enabled[kMaxDevices];
     auto kern = k_int4_back_tile<VT, OT, PLANES, NG, ROWS, KW>;
     static_assert(S::bytes <= kLdsBytes && S::codes >= NG * S::vectors * 4, "two stages, and then what is taken off");
@@ -613,6 +624,7 @@ hipError_t launch_tile(const Args &x) {
 template <typename VT, typename OT, int PLANES, int NG, int VECS, int WAVES>
 hipError_t launch_split_waves(const Args &x) {
     using S = BackSplit<PLANES, NG, VECS>;
+    if (x.name) return put_name<VT, OT>(x, "k_int4_back_split<%s, %s, %d, %d, %d, %d>", PLANES, NG, VECS, WAVES);
     static std::atomic<size_t> enabled[kMaxDevices];
     auto kern = k_int4_back_split<VT, OT, PLANES, NG, VECS, WAVES>;
     constexpr size_t staged = (size_t)WAVES * S::wave_bytes, joined = (size_t)WAVES * (32 * 64 + NG * S::vectors) * 4;
@@ -692,11 +704,8 @@ hipError_t launch(const Args &x) {
     return hipSuccess;
 }
 
-}  // namespace
-
-hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool short_dy,
-                                  float scale, void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo,
-                                  hipStream_t stream) {
+Args args_of(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, float scale, void *out, int batch, int64_t ldv,
+             int64_t ldo, hipStream_t stream) {
     Args x = {};
     x.m[0] = int4_of(a);
     if (b) x.m[1] = int4_of(b);
@@ -713,10 +722,31 @@ hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, 
     x.scale = scale;
     x.out = out;
     x.stream = stream;
+    return x;
+}
+
+hipError_t launch_types(const Args &x, int v_dtype, bool short_dy, int out_dtype) {
     if (v_dtype == RSR_BF16)
         return out_dtype != RSR_BF16 ? launch<uint16_t, float, 3>(x) : launch<uint16_t, uint16_t, 2>(x);
     if (out_dtype != RSR_BF16) return launch<float, float, 3>(x);
     return short_dy ? launch<float, uint16_t, 2>(x) : launch<float, uint16_t, 3>(x);
+}
+
+}  // namespace
+
+hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool short_dy,
+                                  float scale, void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo,
+                                  hipStream_t stream) {
+    return launch_types(args_of(a, b, dy, scale, out, batch, ldv, ldo, stream), v_dtype, short_dy, out_dtype);
+}
+
+void int4_transposed_kernel_name(const rsr_handle_s *a, const rsr_handle_s *b, int v_dtype, bool short_dy, int out_dtype,
+                                 int batch, char *buf, size_t len) {
+    Args x = args_of(a, b, nullptr, 1.0f, nullptr, batch, a->rows * (b ? 2 : 1), a->cols, nullptr);
+    x.name = buf;
+    x.name_len = len;
+    buf[0] = 0;
+    (void)launch_types(x, v_dtype, short_dy, out_dtype);
 }
 
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,

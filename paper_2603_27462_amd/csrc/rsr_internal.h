@@ -183,7 +183,7 @@ hipError_t launch_int4_pack(const rsr_handle_s *h, const int8_t *Q, const float 
                             int64_t group, int *flags);
 hipError_t launch_int4(const rsr_handle_s *h, const void *v, int v_dtype, float scale, void *out, int out_dtype,
                        int batch, int64_t ldv, int64_t ldo, hipStream_t stream);
-void int4_kernel_name(const rsr_handle_s *h, int v_dtype, int batch, char *buf, size_t len);
+void int4_kernel_name(const rsr_handle_s *h, const rsr_handle_s *up, int v_dtype, int batch, char *buf, size_t len);
 hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, const void *v, int v_dtype, int act,
                              void *out, int out_dtype, float *pre, int batch, int64_t ldv, int64_t ldo,
                              hipStream_t stream);
@@ -192,6 +192,8 @@ hipError_t launch_int4_gated(const rsr_handle_s *gate, const rsr_handle_s *up, c
 hipError_t launch_int4_transposed(const rsr_handle_s *a, const rsr_handle_s *b, const void *dy, int v_dtype, bool short_dy,
                                   float scale, void *out, int out_dtype, int batch, int64_t ldv, int64_t ldo,
                                   hipStream_t stream);
+void int4_transposed_kernel_name(const rsr_handle_s *a, const rsr_handle_s *b, int v_dtype, bool short_dy, int out_dtype,
+                                 int batch, char *buf, size_t len);
 hipError_t launch_gated_slopes(const float *pre, const void *dh, int d_dtype, int64_t ldd, int act, int64_t rows,
                                int batch, float *dpre, hipStream_t stream);
 
