@@ -153,10 +153,21 @@ def _load_call(lib) -> None:
 
 
 class Handle:
-    """Owns an rsr_handle_t; freed by rsr_destroy() or garbage collection."""
+    """Owns an rsr_handle_t; freed by rsr_destroy() or garbage collection.  A copy (also of a module around it) is the same
+    handle, and it is not pickled: a second owner of the pointer would free it twice."""
 
     def __init__(self, ptr: int, rows: int, cols: int, k: int, kind: int):
         self.ptr, self.rows, self.cols, self.k, self.kind = ptr, rows, cols, k, kind
+
+    def __copy__(self):
+        return self
+
+    def __deepcopy__(self, memo):
+        return self
+
+    def __reduce__(self):
+        raise TypeError("a handle is not pickled: it points to memory of this process (rsr_serialize makes bytes of it, but "
+                        "not of stacked handles and 4-bit weights)")
 
     def __del__(self):
         try:
