@@ -233,7 +233,7 @@ __global__ __launch_bounds__(few_most_waves(NM) * 64) void k_int4_few(Int4 m0, I
         put(static_cast<float *>(out) + q * ldo + row, result);
 }
 
-// ---- split: up to 64 vectors ---------------------------------------------------------------------------
+// ---- split: five to 32 vectors, and more where an estimate prefers it to tiles (split_us, tile_us) -------------
 // WAVES waves share the columns of G row groups (of each matrix); each stages its own columns of 16 NT vectors, half a tile at
 // a time.  The vectors are the rows of the MFMA: lane l of the result holds row l % 16 of vectors 4 (l / 16) .. + 3.
 // 14336 x 4096, 16 bf16 vectors, groups of 64: 14.8 us (a plain read of the codes 6.5); a step's staging, decoding and scaling are
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES / 4) void k_int4_split(
 // eight waves 299, 128 x 128 in four with stages of 64 columns 429, 32 rows x 128 vectors per wave 302, 64 x 128 per wave with all 512
 // registers 358; the next stage written between or behind the products 277 to 303; sums scaled behind the branches of a stage
 // (where the compiler moves them if it may) spill 700 bytes.  Groups of 32: 392 us, a sum of 32 columns is two MFMAs and 16
-// multiplications.
+// multiplications.  With zero points and groups of 128 three registers do not fit (16 bytes of scratch).
 constexpr int kTileWaves = 4, kTileVecs = 2;  // 64 rows each; blocks of 32 vectors
 
 template <typename VT, int GPT>
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(64 * kTileWaves, 2) void k_int4_tile(
     const int rt = band * 8 + in_band % band_rows, vec0 = in_band / band_rows * S::vectors;
     const Int4 mat[2] = {m0, NM == 2 ? m1 : m0};
 
-    // piece j of this thread: of vector mine + j * kApart, a uniform distance further on (no vector there: zeros)
+    // piece j of this thread: of vector mine + j * kApart, a uniform distance further on (no vector there: the last one again, not stored)
     constexpr int kApart = S::threads / S::pieces;
     const int piece = tid % S::pieces, mine = tid / S::pieces;
     const VT *first = v + (long long)min(vec0 + mine, batch - 1) * ldv + 8 * piece;
@@ -823,7 +823,8 @@ hipError_t launch_all(const Args &x, int group) {
     return group == 32 ? launch_any<VT, 8, NM>(x) : group == 64 ? launch_any<VT, 4, NM>(x) : launch_any<VT, 2, NM>(x);
 }
 
-// (A launch holds fewer than 2^32 threads, at most 512 per row group and 16 vectors, and 65535 sets of vectors: so many at a time.)
+// (A launch holds fewer than 2^32 threads, at most 512 per row group and 16 vectors, and 65535 sets of vectors: so many at a time.  Split with
+// sixteen waves has 1024 per row group, but fewer than 512 workgroups.)
 template <typename VT, int NM>
 hipError_t launch_groups(const Args &x, int group) {
     const long long sets = (1LL << 31) / (512LL * x.ngroups);

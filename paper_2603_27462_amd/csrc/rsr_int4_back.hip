@@ -409,7 +409,7 @@ __global__ __launch_bounds__(256 * KW, 2) void k_int4_back_tile(Int4 m0, Int4 m1
     }
 }
 
-// ---- split: up to 32 vectors -----------------------------------------------------------------------------
+// ---- split: up to 32 vectors, and more where an estimate prefers it to tiles or there are none (launch_all) ------------
 // WAVES waves share the rows of 64 columns; each stages 32 rows of dy, scaled, and their codes in LDS of its own.  Bound by the chain
 // of a step (scales, dy, operands: three turns through LDS) and what is around it: 4096 x 14336, one bf16 vector 17.2 us (1.7 TB/s,
 // a plain read of the codes 6.2; 13.7 with dy s rounded to one plane, and that 22.5 where branches around its requests had all loads
@@ -642,7 +642,8 @@ template <typename VT, typename OT, int PLANES, int NG>
 hipError_t launch_split(const Args &x) {
     if (x.batch > 16) return launch_split_waves<VT, OT, PLANES, NG, 32, 8>(x);
     // sixteen waves where every one gets four steps, and the registers allow it.  Measured, one vector, sixteen / eight: 14336 x 4096
-    // 38.5 / 47.2 us, 4096 x 14336 17.3 / 18.3, 2560 x 6912 in groups of 32 13.1 / 14.2, 1024 x 1024 in groups of 32 7.5 / 7.2
+    // 38.5 / 47.2 us, 4096 x 14336 17.3 / 18.3, 2560 x 6912 in groups of 32 13.1 / 14.2 (with 40 bytes of scratch), 1024 x 1024 in groups
+    // of 32 7.5 / 7.2
     if constexpr (PLANES == 2 && sizeof(VT) == 2)
         if (x.n_rows >= 2048) return launch_split_waves<VT, OT, PLANES, NG, 16, 16>(x);
     return launch_split_waves<VT, OT, PLANES, NG, 16, 8>(x);

@@ -98,7 +98,9 @@ class _Gated(_ReverseMode):
 
 class RsrInt4Linear(torch.nn.Module):
     """y = W x for fixed 4-bit weights, W[r][c] = scales[r][c // group] * (codes[r][c] - zeros[r][c // group]) (see
-    rsr_preprocess_int4); y is of type `dtype`.  x is float32 or bfloat16, of any leading dimensions; its gradient has its type."""
+    rsr_preprocess_int4); y is of type `dtype`.  x is float32 or bfloat16, of any leading dimensions; its gradient has its type.
+    To train on bfloat16, take `dtype=torch.bfloat16` here too: the gradient of a float32 y is multiplied with all of its bits, which
+    takes up to 1.7 times as long (4096 x 14336, 512 tokens 293 us against 171)."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, group: int, zeros=None, dtype=torch.float32):
         super().__init__()
