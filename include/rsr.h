@@ -273,8 +273,8 @@ rsr_handle_t rsr_preprocess_int4(const int8_t *Q, const float *scales, const int
  * a group are scaled.  The transpose sums over the rows, whose scales differ, so there it is the vector that is scaled:
  * in float32, and where v and out are both bf16 it is kept to 16 bits, which hold the product with a bf16 scale exactly
  * and any other to 2^-16; with float32 on either side nothing is rounded below float32.  Every entry is multiplied, zeros too: an infinite or NaN element of a vector
- * leaves none of its results finite (others of the batch are never touched), and elements beyond 2^120 may.  A float32 element below
- * 2^-109 loses its bits below 2^-133.  The order of the sums depends on the number of vectors, as for rsr_matvec_ex; the
+ * leaves none of its results finite (others of the batch are never touched), and elements beyond 2^120 may.  A float32 element (transposed: a
+ * scaled one) below 2^-109 loses its bits below 2^-133.  The order of the sums depends on the number of vectors, as for rsr_matvec_ex; the
  * same call gives the same bits every time.
  *
  * Asynchronous on `stream`, allocates nothing and never synchronises, so it may be captured into a HIP graph; the
